@@ -135,10 +135,10 @@ def _halves(row, octet, purpose, seed):
 
 
 def _uniforms(rows, cols, row0, seed):
-    """The 32-bit uniform word of each element (cols a multiple of 8)."""
+    """The 32-bit uniform word of each element."""
     row = torch.arange(row0, row0 + rows, device="cuda", dtype=torch.int64)[:, None]
-    octet = torch.arange(cols // 8, device="cuda", dtype=torch.int64)[None, :]
-    return (_halves(row, octet, 0, seed) << 16) | _halves(row, octet, 1, seed)
+    octet = torch.arange(-(-cols // 8), device="cuda", dtype=torch.int64)[None, :]
+    return ((_halves(row, octet, 0, seed) << 16) | _halves(row, octet, 1, seed))[:, :cols]
 
 
 def _blocks(x):
@@ -150,28 +150,30 @@ def _blocks(x):
 
 
 def _exponents(mag):
-    """The least e >= -127 with max <= 6 * 2^e of each block, and 128 for a
+    """The least e >= -126 with max <= 6 * 2^e of each block, and 128 for a
     block that holds an infinity or a NaN."""
     top = mag.amax(-1)
     frac, p = torch.frexp(top)
-    e = torch.where(frac <= 0.75, p - 3, p - 2).clamp(min=-127)
-    e = torch.where(top == 0, torch.full_like(e, -127), e)
+    e = torch.where(frac <= 0.75, p - 3, p - 2).clamp(min=-126)
+    e = torch.where(top == 0, torch.full_like(e, -126), e)
     return torch.where(torch.isfinite(top), e, torch.full_like(e, 128))
 
 
-def _magnitudes(mag, e, stochastic, seed, row0=0):
-    """The codes' magnitudes in half units, as 32-bit floats [rows, blocks, 32]."""
+def _magnitudes(mag, e, words=None):
+    """The codes' magnitudes in half units, as 32-bit floats [rows, blocks, 32]:
+    rounded to the nearest, or by each element's uniform word."""
     fine = e < 128
     down = ((127 - torch.where(fine, e, 0)) << 23).to(torch.int32).view(torch.float32)  # 2^-e, by its bits
     y = torch.where(fine[..., None], mag * down[..., None], 0.0)
     step = torch.where(y < 2, 1.0, torch.where(y < 4, 2.0, 4.0))  # of the grid at y, in half units
     q = 2 * y / step
-    if not stochastic:
+    if words is None:
         return torch.round(q) * step
     low = q.floor()
     t = ((q - low) * 4294967296.0).to(torch.int64)
-    r = _uniforms(mag.shape[0], mag.shape[1] * 32, row0, seed).view(mag.shape)
-    return (low + (r < t)) * step
+    r = torch.zeros(mag.shape[0], mag.shape[1] * 32, dtype=torch.int64, device=mag.device)
+    r[:, :words.shape[1]] = words
+    return (low + (r.view(mag.shape) < t)) * step
 
 
 def _power(e):
@@ -180,11 +182,11 @@ def _power(e):
     return torch.where(e < 128, two, math.nan)
 
 
-def _plain_values(x, stochastic, seed):
+def _plain_values(x, words):
     """What the codes of x stand for, in x's type."""
     mag = _blocks(x)
     e = _exponents(mag)
-    half = _magnitudes(mag, e, stochastic, seed)
+    half = _magnitudes(mag, e, words)
     v = (half.double() * (_power(e) / 2)[..., None]).flatten(1)[:, :x.shape[1]]
     return torch.copysign(v, x.double()).to(x.dtype)
 
@@ -202,13 +204,14 @@ def _plain_read(codes, scales, cols):
 def _plain_sum(g, e, seed, worker0):
     """The rows' codes in half units on the shared exponents e, added."""
     mag = _blocks(g)
-    half = _magnitudes(mag, e.expand(g.shape[0], -1), True, seed, worker0).flatten(1)[:, :g.shape[1]]
+    words = _uniforms(g.shape[0], g.shape[1], worker0, seed)
+    half = _magnitudes(mag, e.expand(g.shape[0], -1), words).flatten(1)[:, :g.shape[1]]
     return torch.copysign(half, g).sum(0).to(torch.int32)
 
 
 def _plain_step(g, seed):
     M, d = g.shape
-    e = torch.full((1, -(-d // 32)), -127, dtype=torch.int32, device=g.device)
+    e = torch.full((1, -(-d // 32)), -126, dtype=torch.int32, device=g.device)
     for m in range(M):
         e = torch.maximum(e, _exponents(_blocks(g[m:m + 1])))
     total = torch.zeros(d, dtype=torch.int32, device=g.device)
@@ -256,7 +259,7 @@ def _codes_of(x, codes, scales):
     cols = x.shape[1]
     mag = _blocks(x)
     e = _exponents(mag)
-    half = _magnitudes(mag, e, False, 0).flatten(1)
+    half = _magnitudes(mag, e).flatten(1)
     c = torch.where(half < 4, half, torch.where(half < 8, 2 + half / 2, 4 + half / 4)).to(torch.uint8)
     c[:, :cols] |= torch.signbit(x).to(torch.uint8) << 3
     nb = e.shape[1]
@@ -328,11 +331,12 @@ def run(state):
         return _OWN[op](uq, state, case, TYPE_IDS[case["dtype"]])
     if op == "round trip":
         x = state["x"][:, :case["cols"]]
+        words = _uniforms(case["rows"], case["cols"], 0, state["seed"]) if case["stochastic"] else None
         res = {}
         if case["form"] != "transposed":
-            res["values"] = _plain_values(x, case["stochastic"], state["seed"])
+            res["values"] = _plain_values(x, words)
         if case["form"] != "rows":
-            res["values_t"] = _plain_values(x.t(), case["stochastic"], state["seed"])
+            res["values_t"] = _plain_values(x.t(), None if words is None else words.t())
         return res
     if op == "read":
         return dict(values=_plain_read(state["codes"], state["scales"], case["cols"]).to(DTYPES[case["dtype"]]))
@@ -463,18 +467,18 @@ def _exact_power(e):
 
 
 def _exact_scale(x):
-    """The least e >= -127 with the block's largest magnitude at most 6 * 2^e (finite inputs)."""
+    """The least e >= -126 with the block's largest magnitude at most 6 * 2^e (finite inputs)."""
     r, c = x.shape
     nb = -(-c // 32)
     full = torch.zeros(r, nb * 32, dtype=torch.float64, device=x.device)
     full[:, :c] = x.double().abs()
     top = full.view(r, nb, 32).max(-1).values
-    e = torch.ceil(torch.log2(top / 6)).clamp(min=-127)
+    e = torch.ceil(torch.log2(top / 6)).clamp(min=-126)
     e = e + (top > 6 * _exact_power(e)).double()
-    return e - ((top <= 6 * _exact_power(e - 1)) & (e > -127)).double()
+    return e - ((top <= 6 * _exact_power(e - 1)) & (e > -126)).double()
 
 
-def _exact_round(x, e, stochastic, seed, row0=0):
+def _exact_round(x, e, words=None):
     """The values that the codes of x stand for on the exponents e, in 64 bits."""
     r, c = x.shape
     two = _exact_power(e).repeat_interleave(32, dim=1)[:, :c]
@@ -483,8 +487,8 @@ def _exact_round(x, e, stochastic, seed, row0=0):
     at = (torch.searchsorted(table, y, right=True) - 1).clamp(max=6)
     lo, hi = table[at], table[at + 1]
     part = (y - lo) / (hi - lo)
-    if stochastic:
-        up = _exact_words(r, c, row0, seed) < torch.floor(part * 4294967296.0).to(torch.int64)
+    if words is not None:
+        up = words < torch.floor(part * 4294967296.0).to(torch.int64)
         up |= part >= 1
     else:
         up = (part > 0.5) | ((part == 0.5) & (at % 2 == 1))
@@ -504,12 +508,13 @@ def exact(case, seed):
     op, philox_seed = case["op"], seed * 7919 + 1
     if op == "round trip":
         x = _matrix(case["rows"], case["cols"], case["dtype"], case["pad"], seed)[:, :case["cols"]]
+        words = _exact_words(case["rows"], case["cols"], 0, philox_seed) if case["stochastic"] else None
         res = {}
         if case["form"] != "transposed":
-            res["values"] = _exact_round(x, _exact_scale(x), case["stochastic"], philox_seed)
+            res["values"] = _exact_round(x, _exact_scale(x), words)
         if case["form"] != "rows":
             x = x.t().contiguous()
-            res["values_t"] = _exact_round(x, _exact_scale(x), case["stochastic"], philox_seed)
+            res["values_t"] = _exact_round(x, _exact_scale(x), None if words is None else words.t())
         return res
     if op == "read":
         state = prepare(case, seed)
@@ -527,5 +532,5 @@ def exact(case, seed):
         e = torch.maximum(e, _exact_scale(g[m:m + 1]))
     total = torch.zeros(d, dtype=torch.float64, device="cuda")
     for m in range(M):
-        total += _exact_round(g[m:m + 1], e, True, philox_seed, m)[0]
+        total += _exact_round(g[m:m + 1], e, _exact_words(1, d, m, philox_seed))[0]
     return dict(out=total / M, sum=None, scales=None)
