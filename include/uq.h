@@ -421,6 +421,132 @@ int uq_randk_select_gather(const float* g, int64_t d, int32_t M, int64_t ldg, in
                            float* sub, int64_t lds, float* out, void* ws, size_t ws_bytes, void* stream);
 int uq_scatter_into(const float* vals, const uint32_t* sel, int64_t K, float* out, int64_t d, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Microscaled 4-bit floating point: the format whose products the matrix
+ * cores form directly.  A row's elements lie in blocks of 32 (the last one
+ * filled with zeros); a block has one scale byte, 2^(byte - 127) (255: every
+ * element of the block is NaN), and 32 fields of 4 bits in 16 bytes, low
+ * nibble first: the sign above a 3-bit code 0..7 for the magnitudes 0, 0.5, 1,
+ * 1.5, 2, 3, 4 and 6 (E2M1 elements with an E8M0 scale).
+ *   codes    [rows][ldc] bytes, ldc >= 16 * ceil(cols / 32), ldc % 16 == 0
+ *   scales   [rows][lds] bytes, lds >= ceil(cols / 32), lds % 16 == 0
+ * Both arrays hold whole rows of their leading dimension; 16-byte aligned.
+ * Calls that write them write 16 * ceil(cols / 32) bytes of a row's codes and
+ * ceil(cols / 32) of its scales and leave the rest as it was, and what lies
+ * there never enters a result.
+ *   Scale rule: e is the least integer >= -126 with a <= 6 * 2^e, a the
+ * block's largest |x|; byte = e + 127.  Nothing saturates, so that stochastic
+ * rounding is unbiased.  A block that holds a NaN or an infinity gets byte
+ * 255 and codes 0.
+ *   Rounding: y = 2 |x| / 2^e (at most 12), step = 1, 2 or 4 for y < 4, y < 8
+ * and from 8 on (the grid in half units), q = y / step.  Nearest: q to the nearest
+ * integer, ties to even.  Stochastic: l = floor(q), one more when
+ * r < floor((q - l) * 2^32), with the 32-bit uniform word r of row i ("worker"
+ * i) at column j as above (the arithmetic contract; key = seed).  The field's
+ * sign is x's sign bit, also where the magnitude becomes 0.
+ * ------------------------------------------------------------------------ */
+
+/* Element types of matrices. */
+enum uq_type { UQ_F32 = 0, UQ_BF16 = 1, UQ_F16 = 2 };
+
+/*
+ * Quantises a matrix along its rows, along its columns (the codes of the
+ * transposed matrix, which a backward pass multiplies by), or both from one
+ * read.
+ *   x           [rows][ldx] of `type` (read), ldx >= cols, rows starting
+ *               on 16-byte boundaries (ldx % 4 == 0 for UQ_F32, % 8 otherwise)
+ *   rows, cols  0 .. 2^31 - 1 (0: nothing to do)
+ *   stochastic  0: to the nearest; 1: stochastically, with `seed`
+ *   codes, scales      [rows][ldc], [rows][lds]: the rows' codes (written), or
+ *               both NULL
+ *   codes_t, scales_t  [cols][ldct], [cols][ldst]: the transposed matrix's
+ *               codes (written), its blocks 32 rows of x; or both NULL.  An
+ *               element has the same uniform word in both.
+ * A leading dimension whose array is NULL is ignored.  One pair at least must
+ * be given (UQ_EINVAL); outputs must not overlap x or each other.
+ */
+int uq_mx4_quantize(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ldx, int32_t stochastic,
+                    uint64_t seed, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds, uint8_t* codes_t,
+                    int64_t ldct, uint8_t* scales_t, int64_t ldst, void* stream);
+
+/*
+ * The values that codes stand for, rounded once to `type` (exact in binary32
+ * but for the top scale, 2^127, whose largest elements overflow to infinity).
+ *   codes, scales   as above (read); byte 255 gives NaN
+ *   rows, cols      0 .. 2^31 - 1
+ *   out             [rows][ldo] of `type` (written: cols entries of a row)
+ */
+int uq_mx4_dequantize(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t rows,
+                      int64_t cols, int32_t type, void* out, int64_t ldo, void* stream);
+
+/*
+ * out[i][j] = sum over l < k of A[i][l] * B[j][l] for two matrices held as
+ * codes whose blocks run along l (both operands row by row: B is the second
+ * factor transposed, as a layer's weight [outputs][inputs] lies).  Products of
+ * elements and scales are exact, sums are binary32 in an order that depends
+ * on the sizes alone.  A block of byte 255 makes the outputs of its row or
+ * column NaN.
+ *   a, lda, a_scales, ldas   m x k codes      b, ldb, b_scales, ldbs   n x k codes
+ *   m, n, k      0 .. 2^31 - 1 (k = 0: the sum is 0)
+ *   type         of out
+ *   out          [m][ldo] (written, or read and written), rows on 16-byte
+ *                boundaries
+ *   accumulate   0: out = the product; 1: out += the product, added in
+ *                binary32 and rounded once
+ *   ws           device workspace of at least
+ *                uq_mx4_matmul_workspace_bytes(m, n, k) bytes, 16-byte aligned;
+ *                its contents are scratch
+ * out must not overlap the operands or ws.
+ */
+int uq_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* a_scales, int64_t ldas, const uint8_t* b, int64_t ldb,
+                  const uint8_t* b_scales, int64_t ldbs, int64_t m, int64_t n, int64_t k, int32_t type, void* out,
+                  int64_t ldo, int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes uq_mx4_matmul needs; 0 never returned. */
+size_t uq_mx4_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
+
+/*
+ * The aggregation step on this format: one scale byte for each block of 32
+ * coordinates, shared by the workers by maximum (as the norm is in Algorithm
+ * 1), stochastic codes on the shared bytes, whose half units are integers
+ * (0, 1, 2, 3, 4, 6, 8, 12), an exact integer sum of those, and the mean.
+ *
+ * uq_mx4_shared_scale: the bytes of the largest |g| over the rows; they order
+ * as the magnitudes do (255, a NaN or an infinity in the block, above all), so
+ * that of several calls or ranks the largest byte is the shared one.
+ *   g            [rows][ldg] fp32 (read)
+ *   accumulate   0: scales = the rows' bytes; 1: the larger of those and the
+ *                bytes held
+ *   scales       [ceil(d / 32)] bytes (written, or read and written)
+ */
+int uq_mx4_shared_scale(const float* g, int64_t d, int32_t rows, int64_t ldg, int32_t accumulate, uint8_t* scales,
+                        void* stream);
+
+/*
+ * Codes of `rows` workers on the shared bytes, added into the sum.
+ *   g, rows, ldg, worker0, seed   as for uq_quantize_single
+ *   scales       [ceil(d / 32)] bytes (read), at least those of every row;
+ *                a magnitude beyond 6 * 2^e takes code 7 all the same, and a
+ *                byte of 0 is read as 1
+ *   accumulate   0: sum = the rows' total; 1: sum += the rows' total
+ *   sum          [d] int32 (written, or read and written), in half units of
+ *                the block's scale; 0 is added where the byte is 255
+ *   M, out       NULL: no mean (M is then ignored); else out [d] fp32
+ *                (written): RN32(sum_i * RN32(RN32(1 / M) * 2^(e - 1))), NaN
+ *                where the byte is 255; M >= 1, 12 * M < 2^31
+ */
+int uq_mx4_quantize_sum(const float* g, int64_t d, int32_t rows, int64_t ldg, int32_t worker0, const uint8_t* scales,
+                        uint64_t seed, int32_t accumulate, int32_t* sum, int32_t M, float* out, void* stream);
+
+/*
+ * The whole step over M resident workers in one pass: bit for bit
+ * uq_mx4_shared_scale (accumulate = 0) followed by uq_mx4_quantize_sum over all
+ * rows (worker0 = 0, accumulate = 0, out set).
+ *   M   1 .. 16 (UQ_ERANGE beyond: use the two calls)
+ */
+int uq_mx4_aggregate(const float* g, int64_t d, int32_t M, int64_t ldg, uint64_t seed, uint8_t* scales, int32_t* sum,
+                     float* out, void* stream);
+
 /*
  * Test hook, not part of the aggregation step: caps the grids of the
  * streaming passes (norm, index, quantise, sum, reconstruction) at `blocks`

@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(HERE, "libuq.so")
 UQ_OK, UQ_EINVAL, UQ_ERANGE, UQ_EALIGN, UQ_EWORKSPACE, UQ_EHIP = 0, -1, -2, -3, -4, -5
 UQ_MAX_SCALES = 16
 UQ_NOALLOC_SCRATCH_BYTES = 64 << 20
+UQ_F32, UQ_BF16, UQ_F16 = 0, 1, 2
 
 
 class UQError(RuntimeError):
@@ -74,6 +75,14 @@ def _load() -> ctypes.CDLL:
     L.uq_randk_select_gather.argtypes = [P, i64, i32, i64, i64, u64, P, P, i64, P, P, sz, P]
     L.uq_gather.argtypes = [P, i64, i32, i64, P, i64, P, i64, P]
     L.uq_scatter.argtypes = L.uq_scatter_into.argtypes = [P, P, i64, P, i64, P]
+    L.uq_mx4_quantize.argtypes = [P, i32, i64, i64, i64, i32, u64, P, i64, P, i64, P, i64, P, i64, P]
+    L.uq_mx4_dequantize.argtypes = [P, i64, P, i64, i64, i64, i32, P, i64, P]
+    L.uq_mx4_matmul.argtypes = [P, i64, P, i64, P, i64, P, i64, i64, i64, i64, i32, P, i64, i32, P, sz, P]
+    L.uq_mx4_matmul_workspace_bytes.argtypes = [i64, i64, i64]
+    L.uq_mx4_matmul_workspace_bytes.restype = sz
+    L.uq_mx4_shared_scale.argtypes = [P, i64, i32, i64, i32, P, P]
+    L.uq_mx4_quantize_sum.argtypes = [P, i64, i32, i64, i32, P, u64, i32, P, i32, P, P]
+    L.uq_mx4_aggregate.argtypes = [P, i64, i32, i64, u64, P, P, P, P]
     L.uq_set_grid_cap.argtypes = [i64]
     L.uq_set_randk_mode.argtypes = [i32]
     L.uq_strerror.argtypes = [ctypes.c_int]
@@ -85,7 +94,8 @@ def _load() -> ctypes.CDLL:
                  "uq_sum_packed", "uq_quantize_sum", "uq_quantize_sum_idx4",
                  "uq_index_quantize_sum", "uq_index_quantize", "uq_aggregate",
                  "uq_randk_select", "uq_randk_select_gather", "uq_gather",
-                 "uq_scatter", "uq_scatter_into", "uq_set_grid_cap", "uq_set_randk_mode"):
+                 "uq_scatter", "uq_scatter_into", "uq_mx4_quantize", "uq_mx4_dequantize", "uq_mx4_matmul",
+                 "uq_mx4_shared_scale", "uq_mx4_quantize_sum", "uq_mx4_aggregate", "uq_set_grid_cap", "uq_set_randk_mode"):
         getattr(L, name).restype = ctypes.c_int
     return L
 
@@ -268,6 +278,40 @@ def uq_randk_select_gather(g, d, M, ldg, K, seed, sel, sub, lds, out, ws, ws_byt
 
 def uq_scatter_into(vals, sel, K, out, d, stream=None) -> None:
     _check(lib.uq_scatter_into(_ptr(vals), _ptr(sel), K, _ptr(out), d, _stream(stream)))
+
+
+def uq_mx4_quantize(x, type, rows, cols, ldx, stochastic, seed, codes, ldc, scales, lds, codes_t, ldct, scales_t, ldst,
+                    stream=None) -> None:
+    _check(lib.uq_mx4_quantize(_ptr(x), type, rows, cols, ldx, stochastic, seed, _ptr(codes), ldc, _ptr(scales), lds,
+                               _ptr(codes_t), ldct, _ptr(scales_t), ldst, _stream(stream)))
+
+
+def uq_mx4_dequantize(codes, ldc, scales, lds, rows, cols, type, out, ldo, stream=None) -> None:
+    _check(lib.uq_mx4_dequantize(_ptr(codes), ldc, _ptr(scales), lds, rows, cols, type, _ptr(out), ldo,
+                                 _stream(stream)))
+
+
+def uq_mx4_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
+    return int(lib.uq_mx4_matmul_workspace_bytes(m, n, k))
+
+
+def uq_mx4_matmul(a, lda, a_scales, ldas, b, ldb, b_scales, ldbs, m, n, k, type, out, ldo, accumulate, ws, ws_bytes,
+                  stream=None) -> None:
+    _check(lib.uq_mx4_matmul(_ptr(a), lda, _ptr(a_scales), ldas, _ptr(b), ldb, _ptr(b_scales), ldbs, m, n, k, type,
+                             _ptr(out), ldo, accumulate, _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def uq_mx4_shared_scale(g, d, rows, ldg, accumulate, scales, stream=None) -> None:
+    _check(lib.uq_mx4_shared_scale(_ptr(g), d, rows, ldg, accumulate, _ptr(scales), _stream(stream)))
+
+
+def uq_mx4_quantize_sum(g, d, rows, ldg, worker0, scales, seed, accumulate, sum, M, out, stream=None) -> None:
+    _check(lib.uq_mx4_quantize_sum(_ptr(g), d, rows, ldg, worker0, _ptr(scales), seed, accumulate, _ptr(sum), M,
+                                   _ptr(out), _stream(stream)))
+
+
+def uq_mx4_aggregate(g, d, M, ldg, seed, scales, sum, out, stream=None) -> None:
+    _check(lib.uq_mx4_aggregate(_ptr(g), d, M, ldg, seed, _ptr(scales), _ptr(sum), _ptr(out), _stream(stream)))
 
 
 def uq_strerror(status: int) -> str:

@@ -11,7 +11,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
-SOURCES = [os.path.join(CSRC, f) for f in ("uq_kernels.hip", "uq_randk.hip", "uq_abi.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in ("uq_kernels.hip", "uq_randk.hip", "uq_mx4.hip", "uq_mx4_matmul.hip",
+                                             "uq_abi.hip")]
 LIB_PATH = os.path.join(HERE, "libuq.so")
 # achievable-bandwidth references used by the benchmark (not part of libuq)
 PROBE_SOURCES = [os.path.join(CSRC, "uq_probe.hip")]

@@ -636,6 +636,155 @@ int uq_scatter_into(const float* vals, const uint32_t* sel, int64_t K, float* ou
     return scatter(vals, sel, K, out, d, false, stream);
 }
 
+// The codes and scale bytes of a rows x cols matrix in 4-bit floating point.
+static int check_mx4(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t rows, int64_t cols,
+                     const char* codes_name, const char* scales_name)
+{
+    const int64_t blocks = rows > 0 ? (cols + 31) / 32 : 0;
+    UQ_TRY(check_rows(codes, 16 * blocks, rows, ldc, 16, codes_name));
+    return check_rows(scales, blocks, rows, lds, 16, scales_name);
+}
+
+static int check_extent(int64_t v, const char* name)
+{
+    if (v < 0)
+        return fail(UQ_EINVAL, "%s = %lld is negative", name, (long long)v);
+    if (v > 0x7FFFFFFF)
+        return fail(UQ_ERANGE, "%s = %lld exceeds 2^31 - 1", name, (long long)v);
+    return UQ_OK;
+}
+
+static int check_type(int32_t type)
+{
+    if (type != UQ_F32 && type != UQ_BF16 && type != UQ_F16)
+        return fail(UQ_ERANGE, "type = %d is not UQ_F32, UQ_BF16 or UQ_F16", type);
+    return UQ_OK;
+}
+
+// A rows x cols matrix of `type`, rows on 16-byte boundaries.
+static int check_matrix(const void* p, int32_t type, int64_t rows, int64_t cols, int64_t ld, const char* name)
+{
+    return check_rows(p, rows > 0 ? cols : 0, rows, ld, type == UQ_F32 ? 4 : 8, name);
+}
+
+int uq_mx4_quantize(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ldx, int32_t stochastic,
+                    uint64_t seed, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds, uint8_t* codes_t,
+                    int64_t ldct, uint8_t* scales_t, int64_t ldst, void* stream)
+{
+    UQ_TRY(check_type(type));
+    UQ_TRY(check_extent(rows, "rows"));
+    UQ_TRY(check_extent(cols, "cols"));
+    if (stochastic != 0 && stochastic != 1)
+        return fail(UQ_EINVAL, "stochastic must be 0 or 1");
+    if ((codes == nullptr) != (scales == nullptr) || (codes_t == nullptr) != (scales_t == nullptr))
+        return fail(UQ_EINVAL, "codes and scales are given together or are both NULL");
+    if (codes == nullptr && codes_t == nullptr && rows > 0 && cols > 0)
+        return fail(UQ_EINVAL, "neither codes nor codes_t is given");
+    UQ_TRY(check_matrix(x, type, rows, cols, ldx, "x"));
+    if (codes != nullptr)
+        UQ_TRY(check_mx4(codes, ldc, scales, lds, rows, cols, "codes", "scales"));
+    if (codes_t != nullptr)
+        UQ_TRY(check_mx4(codes_t, ldct, scales_t, ldst, cols, rows, "codes_t", "scales_t"));
+    return launched(uq::launch_mx4_quantize(x, type, rows, cols, ldx, stochastic != 0, seed, codes, ldc, scales, lds,
+                                            codes_t, ldct, scales_t, ldst, static_cast<hipStream_t>(stream)));
+}
+
+int uq_mx4_dequantize(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t rows,
+                      int64_t cols, int32_t type, void* out, int64_t ldo, void* stream)
+{
+    UQ_TRY(check_type(type));
+    UQ_TRY(check_extent(rows, "rows"));
+    UQ_TRY(check_extent(cols, "cols"));
+    UQ_TRY(check_mx4(codes, ldc, scales, lds, rows, cols, "codes", "scales"));
+    UQ_TRY(check_matrix(out, type, rows, cols, ldo, "out"));
+    return launched(uq::launch_mx4_dequantize(codes, ldc, scales, lds, rows, cols, type, out, ldo,
+                                              static_cast<hipStream_t>(stream)));
+}
+
+size_t uq_mx4_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k)
+{
+    const int64_t most = 0x7FFFFFFF;
+    return uq::mx4_matmul_workspace_bytes(m < 0 ? 0 : m > most ? most : m, n < 0 ? 0 : n > most ? most : n,
+                                          k < 0 ? 0 : k > most ? most : k);
+}
+
+int uq_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* a_scales, int64_t ldas, const uint8_t* b, int64_t ldb,
+                  const uint8_t* b_scales, int64_t ldbs, int64_t m, int64_t n, int64_t k, int32_t type, void* out,
+                  int64_t ldo, int32_t accumulate, void* ws, size_t ws_bytes, void* stream)
+{
+    UQ_TRY(check_type(type));
+    UQ_TRY(check_extent(m, "m"));
+    UQ_TRY(check_extent(n, "n"));
+    UQ_TRY(check_extent(k, "k"));
+    if (accumulate != 0 && accumulate != 1)
+        return fail(UQ_EINVAL, "accumulate must be 0 or 1");
+    UQ_TRY(check_mx4(a, lda, a_scales, ldas, m, k, "a", "a_scales"));
+    UQ_TRY(check_mx4(b, ldb, b_scales, ldbs, n, k, "b", "b_scales"));
+    UQ_TRY(check_matrix(out, type, m, n, ldo, "out"));
+    if (ws == nullptr)
+        return fail(UQ_EINVAL, "ws is NULL");
+    if (!aligned(ws, 16))
+        return fail(UQ_EALIGN, "ws is not 16-byte aligned");
+    if (ws_bytes < uq_mx4_matmul_workspace_bytes(m, n, k))
+        return fail(UQ_EWORKSPACE, "workspace of %zu bytes is smaller than the %zu needed", ws_bytes,
+                    uq_mx4_matmul_workspace_bytes(m, n, k));
+    return launched(uq::launch_mx4_matmul(a, lda, a_scales, ldas, b, ldb, b_scales, ldbs, m, n, k, type, out, ldo,
+                                          accumulate, ws, static_cast<hipStream_t>(stream)));
+}
+
+int uq_mx4_shared_scale(const float* g, int64_t d, int32_t rows, int64_t ldg, int32_t accumulate, uint8_t* scales,
+                        void* stream)
+{
+    UQ_TRY(check_dims(d, rows, "rows"));
+    UQ_TRY(check_rows(g, d, rows, ldg, 4, "g"));
+    if (accumulate != 0 && accumulate != 1)
+        return fail(UQ_EINVAL, "accumulate must be 0 or 1");
+    UQ_TRY(check_vec(scales, d, "scales"));
+    return launched(
+        uq::launch_mx4_shared_scale(g, d, rows, ldg, accumulate, scales, static_cast<hipStream_t>(stream)));
+}
+
+// The step's arguments after the gradients; has_out: M and out are checked.
+static int check_mx4_sum(int64_t d, const uint8_t* scales, const int32_t* sum, int32_t M, bool has_out,
+                         const float* out)
+{
+    UQ_TRY(check_vec(scales, d, "scales"));
+    UQ_TRY(check_vec(sum, d, "sum"));
+    if (!has_out)
+        return UQ_OK;
+    if (M < 1)
+        return fail(UQ_EINVAL, "M = %d is smaller than 1", M);
+    if (int64_t(12) * M >= int64_t(1) << 31)
+        return fail(UQ_ERANGE, "12 * M >= 2^31 (int32 sums could overflow)");
+    return check_vec(out, d, "out");
+}
+
+int uq_mx4_quantize_sum(const float* g, int64_t d, int32_t rows, int64_t ldg, int32_t worker0, const uint8_t* scales,
+                        uint64_t seed, int32_t accumulate, int32_t* sum, int32_t M, float* out, void* stream)
+{
+    UQ_TRY(check_dims(d, rows, "rows"));
+    UQ_TRY(check_rows(g, d, rows, ldg, 4, "g"));
+    if (worker0 < 0 || static_cast<int64_t>(worker0) + rows > (int64_t(1) << 31))
+        return fail(UQ_ERANGE, "worker ids %d .. %lld exceed [0, 2^31)", worker0, (long long)worker0 + rows - 1);
+    if (accumulate != 0 && accumulate != 1)
+        return fail(UQ_EINVAL, "accumulate must be 0 or 1");
+    UQ_TRY(check_mx4_sum(d, scales, sum, M, out != nullptr, out));
+    return launched(uq::launch_mx4_quantize_sum(g, d, rows, ldg, worker0, scales, seed, accumulate, sum, M, out,
+                                                static_cast<hipStream_t>(stream)));
+}
+
+int uq_mx4_aggregate(const float* g, int64_t d, int32_t M, int64_t ldg, uint64_t seed, uint8_t* scales, int32_t* sum,
+                     float* out, void* stream)
+{
+    UQ_TRY(check_dims(d, M, "M"));
+    UQ_TRY(check_rows(g, d, M, ldg, 4, "g"));
+    if (M > 16)
+        return fail(UQ_ERANGE, "M = %d exceeds 16 resident rows", M);
+    UQ_TRY(check_mx4_sum(d, scales, sum, M, true, out));
+    return launched(
+        uq::launch_mx4_aggregate(g, d, M, ldg, seed, scales, sum, out, static_cast<hipStream_t>(stream)));
+}
+
 int uq_set_randk_mode(int32_t mode)
 {
     if (!uq::set_randk_mode(mode))

@@ -2408,7 +2408,7 @@ bool set_one_shot_cap(int64_t blocks)
     return true;
 }
 
-static int64_t one_shot_cap()
+int64_t one_shot_cap()
 {
     return g_one_shot_cap.load(std::memory_order_relaxed);
 }

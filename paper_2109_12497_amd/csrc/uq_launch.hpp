@@ -126,6 +126,7 @@ int64_t grid_cap();
 // kMinOneShotCap, by the test hook.  Returns false for a value out of range.
 constexpr int64_t kMinOneShotCap = 8;
 bool set_one_shot_cap(int64_t blocks);
+int64_t one_shot_cap();
 
 // ws: at least uq_workspace_bytes(d, M) bytes (norm partials, or the fused
 // path's layout); idx_bits as for launch_quant_sum
@@ -187,5 +188,24 @@ hipError_t launch_scatter(const float* vals, const uint32_t* sel, int64_t K, flo
                           hipStream_t stream);
 hipError_t launch_dequant(const int32_t* sum, int64_t d, int32_t M, const float* w, const ScaleSet& S,
                           const uint8_t* idx, float* out, hipStream_t stream);
+
+// Microscaled 4-bit floating point.  type: an enum uq_type; codes (codes_t)
+// null: the rows' (the transposed matrix's) codes are not formed.
+hipError_t launch_mx4_quantize(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ldx, bool stochastic,
+                               uint64_t seed, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds,
+                               uint8_t* codes_t, int64_t ldct, uint8_t* scales_t, int64_t ldst, hipStream_t stream);
+hipError_t launch_mx4_dequantize(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t rows,
+                                 int64_t cols, int32_t type, void* out, int64_t ldo, hipStream_t stream);
+size_t mx4_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
+hipError_t launch_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* as, int64_t ldas, const uint8_t* b,
+                             int64_t ldb, const uint8_t* bs, int64_t ldbs, int64_t m, int64_t n, int64_t k,
+                             int32_t type, void* out, int64_t ldo, int32_t accumulate, void* ws, hipStream_t stream);
+hipError_t launch_mx4_shared_scale(const float* g, int64_t d, int32_t rows, int64_t ldg, int32_t accumulate,
+                                   uint8_t* scales, hipStream_t stream);
+hipError_t launch_mx4_quantize_sum(const float* g, int64_t d, int32_t rows, int64_t ldg, int32_t worker0,
+                                   const uint8_t* scales, uint64_t seed, int32_t accumulate, int32_t* sum, int32_t M,
+                                   float* out, hipStream_t stream);
+hipError_t launch_mx4_aggregate(const float* g, int64_t d, int32_t M, int64_t ldg, uint64_t seed, uint8_t* scales,
+                                int32_t* sum, float* out, hipStream_t stream);
 
 }  // namespace uq
