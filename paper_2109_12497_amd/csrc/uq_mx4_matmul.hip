@@ -1,6 +1,8 @@
 // The product of two microscaled 4-bit matrices (include/uq.h): the matrix
 // cores multiply the 4-bit fields, apply both scale bytes and accumulate in
 // binary32.
+#include <type_traits>
+
 #include "uq_launch.hpp"
 #include "uq_mx4.hpp"
 
@@ -10,7 +12,61 @@ namespace {
 typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kFp4 = 4;  // the matrix instructions' operand format
+constexpr int kBatch = 4;  // stages of 256 along k whose scale bytes a tile loads together
+
+// Which form a product takes; it goes by the sizes alone, and so does the
+// order of its sums.
+struct MatmulPlan {
+    enum Form { kRows1, kRows2, kRows4, kTiles128, kTiles256 } form;
+    int32_t parts;  // of k, added afterwards (tiles)
+};
+
+// Nanoseconds that tiles of 128 x 128 or 256 x 256 take, `stages` stages of 256
+// deep.  Fitted on one MI355X to within 15%: a compute unit holds two small
+// tiles, which take 0.75 us a stage alone and 1.3 together, with 4 us around
+// them (256 x 8192 x 8192, 2048^3, 4096^3); a large one takes 1.3 us alone and
+// 1.8 with all compute units at work, which then run slower, with 8 us around
+// it (8192^3 269 us in large tiles, 4096^3 41 in large and 49 in small ones,
+// 2048^3 19 and 11).
+int64_t tiles_ns(int64_t m, int64_t n, int64_t stages, int64_t parts, bool large)
+{
+    if (large) {
+        const int64_t blocks = ((m + 255) / 256) * ((n + 255) / 256);
+        const int64_t stage = 1300 + 500 * (blocks < 256 ? blocks : 256) / 256;
+        return (blocks + 255) / 256 * (stages * stage + 8000);
+    }
+    const int64_t blocks = ((m + 127) / 128) * ((n + 127) / 128) * parts, rest = blocks % 512;
+    int64_t ns = blocks / 512 * (stages * 1300 + 4000);
+    if (rest > 0)
+        ns += stages * (rest <= 256 ? 750 : 1300) + 4000;
+    // the parts are written, read again by another launch, and added: 1024 x
+    // 1024 x 32768 88 us in one part, 37 in four
+    return parts > 1 ? ns + 6000 + m * n * 8 * parts / 6000 : ns;
+}
+
+MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
+{
+    if (m <= 16 || k == 0)
+        return {MatmulPlan::kRows1, 1};
+    // 37 x 10001 x 5003 13.3 us in twos, 16.6 in ones
+    if (m <= 32)
+        return {MatmulPlan::kRows2, 1};
+    // 64 x 8192 x 8192 16.4 us in fours, 21.6 in ones, 26.4 in tiles
+    if (m <= 64)
+        return {MatmulPlan::kRows4, 1};
+    const int64_t stages = (k + 255) / 256, batches = (stages + kBatch - 1) / kBatch;
+    MatmulPlan best = {MatmulPlan::kTiles256, 1};
+    int64_t least = tiles_ns(m, n, stages, 1, true);
+    for (int32_t parts = 1; parts <= 8 && parts <= batches; parts *= 2) {
+        const int64_t deep = parts == 1 ? stages : (batches + parts - 1) / parts * kBatch;
+        const int64_t ns = tiles_ns(m, n, deep, parts, false);
+        if (ns < least) {
+            least = ns;
+            best = {MatmulPlan::kTiles128, parts};
+        }
+    }
+    return best;
+}
 
 template <int T>
 __device__ __forceinline__ void store_out(void* out, int64_t at, float v, bool accumulate)
@@ -27,73 +83,596 @@ __device__ __forceinline__ void store_out(void* out, int64_t at, float v, bool a
     }
 }
 
+// Columns col .. col + 3 (a multiple of 4) of the row that starts at `row`.
+template <int T>
+__device__ __forceinline__ void store_four(void* out, int64_t row, int64_t col, int64_t n, f32x4 v, bool accumulate)
+{
+    if (col + 4 > n) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (col + j < n)
+                store_out<T>(out, row + col + j, v[j], accumulate);
+        return;
+    }
+    if constexpr (T == kF32) {
+        f32x4* o = reinterpret_cast<f32x4*>(static_cast<float*>(out) + row + col);
+        *o = accumulate ? *o + v : v;
+    } else {
+        u32x2* o = reinterpret_cast<u32x2*>(static_cast<uint16_t*>(out) + row + col);
+        if constexpr (T == kBF16) {
+            if (accumulate) {
+                const u32x2 old = *o;
+                v += f32x4{__uint_as_float(old[0] << 16), __uint_as_float(old[0] & 0xFFFF0000u),
+                           __uint_as_float(old[1] << 16), __uint_as_float(old[1] & 0xFFFF0000u)};
+            }
+            const bf16x2 a = {static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1])};
+            const bf16x2 b = {static_cast<__bf16>(v[2]), static_cast<__bf16>(v[3])};
+            *o = u32x2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
+        } else {
+            if (accumulate) {
+                const uint32_t o0 = (*o)[0], o1 = (*o)[1];
+                const f16x2 a = __builtin_bit_cast(f16x2, o0), b = __builtin_bit_cast(f16x2, o1);
+                v += f32x4{static_cast<float>(a[0]), static_cast<float>(a[1]), static_cast<float>(b[0]),
+                           static_cast<float>(b[1])};
+            }
+            const f16x2 a = {static_cast<_Float16>(v[0]), static_cast<_Float16>(v[1])};
+            const f16x2 b = {static_cast<_Float16>(v[2]), static_cast<_Float16>(v[3])};
+            *o = u32x2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
+        }
+    }
+}
+
 __device__ __forceinline__ i32x8 operand(i32x4 v)
 {
     return i32x8{v[0], v[1], v[2], v[3], 0, 0, 0, 0};
 }
 
-// One wave per 32 x 32 outputs: lane l holds row l % 32 of both operands and
-// every second block of 32 along k.
-template <int T>
-__global__ __launch_bounds__(kBlock) void k_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* as, int64_t ldas,
-                                                       const uint8_t* b, int64_t ldb, const uint8_t* bs, int64_t ldbs,
-                                                       int64_t m, int64_t n, int64_t nkb, void* out, int64_t ldo,
-                                                       int32_t accumulate, int64_t tile0, int64_t tiles_n)
+// ---------------------------------------------------------------------------
+// Tiles staged through LDS.
+// ---------------------------------------------------------------------------
+constexpr int kStageBlocks = 8;                             // blocks of 32 along k in a stage
+constexpr int kStageBytes = kStageBlocks * kMxBlockBytes;   // of one row's codes: a cache line
+constexpr uint32_t kPast = 0x80000000u;                     // a buffer offset past every operand (reads as 0)
+
+__device__ __forceinline__ i32x4 buffer_of(const uint8_t* p, int64_t bytes)
 {
-    const int64_t tile = tile0 + blockIdx.x;
-    const int64_t tm = tile / tiles_n, tn = tile - tm * tiles_n;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row = tm * 64 + (wave >> 1) * 32 + (lane & 31), col = tn * 64 + (wave & 1) * 32 + (lane & 31);
-    const bool row_ok = row < m, col_ok = col < n;
-    f32x16 acc = {};
-    for (int64_t kb = lane >> 5; kb < ((nkb + 1) & ~int64_t(1)); kb += 2) {
-        i32x4 va = {0, 0, 0, 0}, vb = {0, 0, 0, 0};
-        int sa = 127, sb = 127;
-        if (row_ok && kb < nkb) {
-            va = *reinterpret_cast<const i32x4*>(a + row * lda + kb * kMxBlockBytes);
-            sa = as[row * ldas + kb];
-        }
-        if (col_ok && kb < nkb) {
-            vb = *reinterpret_cast<const i32x4*>(b + col * ldb + kb * kMxBlockBytes);
-            sb = bs[col * ldbs + kb];
-        }
-        acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(va), operand(vb), acc, kFp4, kFp4, 0, sa, 0, sb);
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    return i32x4{static_cast<int>(at), static_cast<int>((at >> 32) & 0xFFFF), static_cast<int>(bytes > 0 ? bytes : 0),
+                 0x00027000};
+}
+
+// Loads straight into LDS: lane i's 16 (4) bytes go to lds + 16 i (4 i).
+// They have no register results; the waits on them are the caller's
+// (vmcnt), and the compiler, which does not know of them, can only wait for
+// more than it needs.  The s_nop is the wait state between a write of m0 and
+// a load that uses it.
+__device__ __forceinline__ void load_lds16(i32x4 r, uint32_t off, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(r)
+                 : "memory");
+}
+__device__ __forceinline__ void load_lds4(i32x4 r, uint32_t off, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(r)
+                 : "memory");
+}
+
+struct MatmulArgs {
+    const uint8_t *a, *as, *b, *bs;
+    int64_t lda, ldas, ldb, ldbs;
+    int64_t m, n, nkb;
+    void* out;
+    int64_t ldo;
+    int32_t accumulate;
+    int32_t tiles_m, tiles_n;
+    int64_t part_blocks;  // blocks along k of a part (all of them: one part)
+    int64_t part_bytes;   // between the parts' outputs
+    int32_t first;        // the launch's first block
+};
+
+// Block -> tile.  Blocks go to the eight XCDs in turn, and each XCD has its
+// own L2: an XCD's blocks take a run of tiles, and a run goes down kBand tiles
+// of a column before it goes to the next, so that the 32 blocks an XCD holds
+// at a time share 8 bands of rows and 4 of columns.
+constexpr int kXcds = 8, kBand = 8;
+
+__device__ __forceinline__ void place(int block, int tiles_m, int tiles_n, int* tm, int* tn)
+{
+    const int all = tiles_m * tiles_n, per = all / kXcds, more = all % kXcds, xcd = block % kXcds;
+    const int tile = xcd * per + (xcd < more ? xcd : more) + block / kXcds;
+    const int band = tile / (kBand * tiles_n), first = band * kBand;
+    const int high = tiles_m - first < kBand ? tiles_m - first : kBand, in = tile - first * tiles_n;
+    *tn = in / high;
+    *tm = first + (in - *tn * high);
+}
+
+// One operand in LDS.  A stage's codes are ROWS rows of kStageBytes, the
+// 16-byte piece c of row r at slot c ^ ((r / 2) & 7): sixteen rows of one
+// piece then lie in all the banks.  Scale bytes come a batch of four stages at
+// a time, ROWS rows of 32 bytes (loads of a row's 8 bytes of each stage cost
+// as much time as the codes, for they touch as many lines: 1.01 us a stage of
+// 256 + 256 rows against 0.58 without), piece p of row r at slot
+// p ^ ((r / 8) & 1).
+constexpr int kBatchBytes = kBatch * kStageBlocks;
+
+template <int ROWS, int W>
+struct Operand {
+    static constexpr int kCodes = ROWS * kStageBytes, kScales = ROWS * kBatchBytes;
+    static constexpr int kStep = 8 * W, kLoads = ROWS / kStep;                  // of a wave, a stage's codes
+    static constexpr int kScaleStep = 32 * W, kScaleLoads = ROWS / kScaleStep;  // and a batch's scales
+    static_assert(ROWS % kScaleStep == 0, "a wave loads the scales of 32 rows at a time");
+
+    const uint8_t *p, *s;
+    uint32_t ld, ld_s, to, to_s;  // to, to_s: where this wave's parts go in LDS
+    int64_t bytes, bytes_s;       // of the rows there are; the rest read as 0
+    uint32_t off, off_s;
+
+    __device__ __forceinline__ Operand(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds,
+                                       int64_t row0, int64_t rows, int64_t kb0, uint32_t lds_codes,
+                                       uint32_t lds_scales, int wave, int lane)
+    {
+        const int64_t have = rows - row0 < ROWS ? rows - row0 : ROWS;
+        p = codes + row0 * ldc + kb0 * kMxBlockBytes;
+        s = scales + row0 * lds + kb0;
+        ld = static_cast<uint32_t>(ldc);
+        ld_s = static_cast<uint32_t>(lds);
+        bytes = have * ldc - kb0 * kMxBlockBytes;
+        bytes_s = have * lds - kb0;
+        const int row = wave * 8 + (lane >> 3), srow = wave * 32 + (lane >> 1);
+        off = row * ld + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
+        off_s = srow * ld_s + (((lane & 1) ^ ((srow >> 3) & 1)) << 4);
+        to = lds_codes + wave * 8 * kStageBytes;
+        to_s = lds_scales + wave * 32 * kBatchBytes;
     }
-    if (!col_ok)
-        return;
+    // Blocks past the last (nkb) read as 0.
+    __device__ __forceinline__ uint32_t offset(int64_t kb, int64_t nkb, int wave, int lane) const
+    {
+        const int row = wave * 8 + (lane >> 3), c = (lane & 7) ^ ((row >> 1) & 7);
+        return kb + c < nkb ? off : kPast;
+    }
+    __device__ __forceinline__ i32x4 codes_from(int64_t kb) const
+    {
+        return buffer_of(p + kb * kMxBlockBytes, bytes - kb * kMxBlockBytes);
+    }
+    __device__ __forceinline__ i32x4 scales_from(int64_t kb) const
+    {
+        return buffer_of(s + kb, bytes_s - kb);
+    }
+
+    static __device__ __forceinline__ i32x4 piece(const uint8_t* lds, int row, int c)
+    {
+        return *reinterpret_cast<const i32x4*>(lds + row * kStageBytes + ((c ^ ((row >> 1) & 7)) << 4));
+    }
+    static __device__ __forceinline__ uint32_t scale(const uint8_t* lds, int row, int stage, int half)
+    {
+        const int slot = ((stage >> 1) & 1) ^ ((row >> 3) & 1);
+        return *reinterpret_cast<const uint32_t*>(lds + row * kBatchBytes + slot * 16 + (stage & 1) * 8 + half * 4);
+    }
+};
+
+// A block of four waves, two by two, forms a tile of 64 FM x 64 FN outputs;
+// a wave holds FM x FN accumulators of 32 x 32.  Lane l holds row l % 32 of
+// an operand's fragment and the blocks 4 (l / 32) + t of a stage for its
+// instruction t = 0..3: any order of the blocks along k gives the same
+// products as long as both operands keep to it, and in this one a lane's four
+// scale bytes are one dword.
+template <int T, int WM, int WN, int FM, int FN>
+__global__ __launch_bounds__(64 * WM * WN, 1) void k_mx4_tiles(MatmulArgs g)
+{
+    constexpr int W = WM * WN, BM = 32 * WM * FM, BN = 32 * WN * FN;
+    using A = Operand<BM, W>;
+    using B = Operand<BN, W>;
+    constexpr int kStage = A::kCodes + B::kCodes, kScaleBatch = A::kScales + B::kScales;
+    __shared__ __attribute__((aligned(128))) uint8_t smem[2 * (kStage + kScaleBatch)];
+    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
+        (__attribute__((address_space(3))) uint8_t*)smem));
+    constexpr int kScalesAt = 2 * kStage;
+
+    const int tiles = g.tiles_m * g.tiles_n, block = g.first + blockIdx.x, part = block / tiles;
+    int tm, tn;
+    place(block - part * tiles, g.tiles_m, g.tiles_n, &tm, &tn);
+    const int64_t kb0 = part * g.part_blocks;
+    const int64_t nkb = g.nkb - kb0 < g.part_blocks ? g.nkb - kb0 : g.part_blocks;
+    char* const out = static_cast<char*>(g.out) + part * g.part_bytes;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t row0 = int64_t(tm) * BM, col0 = int64_t(tn) * BN;
+    const int wm = wave / WN, wn = wave % WN, half = lane >> 5;
+    const int ar = wm * 32 * FM + (lane & 31), br = wn * 32 * FN + (lane & 31);
+    const A a(g.a, g.lda, g.as, g.ldas, row0, g.m, kb0, lds0, lds0 + kScalesAt, wave, lane);
+    const B b(g.b, g.ldb, g.bs, g.ldbs, col0, g.n, kb0, lds0 + A::kCodes, lds0 + kScalesAt + A::kScales, wave, lane);
+    const int64_t stages = (nkb + kStageBlocks - 1) / kStageBlocks;
+
+    // The loads of stage `stage`'s codes, one at a time.
+    struct Codes {
+        i32x4 ra, rb;
+        uint32_t oa, ob, buf;
+    };
+    const auto codes_of = [&](int64_t stage) {
+        const int64_t kb = stage * kStageBlocks;
+        return Codes{a.codes_from(kb), b.codes_from(kb), a.offset(kb, nkb, wave, lane), b.offset(kb, nkb, wave, lane),
+                     static_cast<uint32_t>(stage & 1) * kStage};
+    };
+    const auto load_codes = [&](const Codes& c, int j) {
+        if (j < A::kLoads)
+            load_lds16(c.ra, c.oa + j * A::kStep * a.ld, a.to + c.buf + j * A::kStep * kStageBytes);
+        else
+            load_lds16(c.rb, c.ob + (j - A::kLoads) * B::kStep * b.ld,
+                       b.to + c.buf + (j - A::kLoads) * B::kStep * kStageBytes);
+    };
+    // Load i of the scales of batch `batch`.
+    constexpr int kScaleLoads = A::kScaleLoads + B::kScaleLoads;
+    static_assert(kScaleLoads <= kBatch, "a batch's scales are loaded one a stage");
+    const auto load_scales = [&](int64_t batch, int i) {
+        const int64_t kb = batch * kBatchBytes;
+        const bool of_b = i >= A::kScaleLoads;
+        const int j = of_b ? i - A::kScaleLoads : i;
+        const uint32_t buf = static_cast<uint32_t>(batch & 1) * kScaleBatch;
+        load_lds16(of_b ? b.scales_from(kb) : a.scales_from(kb),
+                   of_b ? b.off_s + j * B::kScaleStep * b.ld_s : a.off_s + j * A::kScaleStep * a.ld_s,
+                   (of_b ? b.to_s : a.to_s) + buf + j * A::kScaleStep * kBatchBytes);
+    };
+    // every load into LDS and every read of it by this wave is done, then the
+    // other waves' are
+    const auto sync = [] {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    f32x16 acc[FM][FN] = {};
+    i32x4 fa[2][FM], fb[2][FN];
+    uint32_t sa[2][FM], sb[2][FN];
+    const auto read_a = [&](int64_t stage, int t, int i) {
+        return A::piece(smem + (stage & 1) * kStage, ar + 32 * i, 4 * half + t);
+    };
+    const auto read_b = [&](int64_t stage, int t, int j) {
+        return B::piece(smem + (stage & 1) * kStage + A::kCodes, br + 32 * j, 4 * half + t);
+    };
+    const auto read_scales = [&](int64_t stage, uint32_t(&xa)[FM], uint32_t(&xb)[FN]) {
+        const uint8_t* l = smem + kScalesAt + ((stage / kBatch) & 1) * kScaleBatch;
+        const int at = static_cast<int>(stage % kBatch);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const int64_t i = tm * 64 + (wave >> 1) * 32 + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
-        if (i < m)
-            store_out<T>(out, i * ldo + col, acc[r], accumulate != 0);
+        for (int i = 0; i < FM; ++i)
+            xa[i] = A::scale(l, ar + 32 * i, at, half);
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+            xb[j] = B::scale(l + A::kScales, br + 32 * j, at, half);
+    };
+    // Bytes of blocks past the last (their codes are 0) must not be NaN's.
+    const auto keep_scales = [&](int64_t stage, uint32_t(&xa)[FM], uint32_t(&xb)[FN]) {
+        const int64_t left = nkb - stage * kStageBlocks - 4 * half;
+        const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+            xa[i] &= keep;
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+            xb[j] &= keep;
+    };
+
+    // A stage is four instructions' depth; each is cut into FM groups of FN
+    // instructions, with a group's share of the next depth's reads and of the
+    // loads of the stage after next between them: a wave waits for its loads
+    // to be taken, so they are spread.  They go into the half of LDS that the
+    // current stage leaves at its fourth depth, start there and end two depths
+    // into the next stage.  Stages past the last read as zeros, past every
+    // operand's end, and enter no product.
+    constexpr int kLoads = A::kLoads + B::kLoads, kSlots = 3 * FM, kPer = (kLoads + kSlots - 1) / kSlots;
+    Codes next = codes_of(0);
+#pragma unroll
+    for (int i = 0; i < kScaleLoads; ++i)
+        load_scales(0, i);
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l)
+        load_codes(next, l);
+    sync();
+    next = codes_of(1);
+    load_scales(1, 0);
+#pragma unroll
+    for (int l = 0; l < kLoads && l < FM * kPer; ++l)  // what a stage before would have loaded at its fourth depth
+        load_codes(next, l);
+    read_scales(0, sa[0], sb[0]);
+    keep_scales(0, sa[0], sb[0]);
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+        fa[0][i] = read_a(0, 0, i);
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+        fb[0][j] = read_b(0, 0, j);
+    const auto depth = [&](auto sub, int64_t s) {
+        constexpr int t = decltype(sub)::value, tn = (t + 1) & 3;
+        const int64_t from = t == 3 ? s + 1 : s;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            fa[tn & 1][i] = read_a(from, tn, i);
+#pragma unroll
+            for (int j = i * FN / FM; j < (i + 1) * FN / FM; ++j)
+                fb[tn & 1][j] = read_b(from, tn, j);
+            if (t != 2) {
+                const int slot = ((t + 1) & 3) * FM + i;
+#pragma unroll
+                for (int l = slot * kPer; l < (slot + 1) * kPer && l < kLoads; ++l)
+                    load_codes(next, l);
+            }
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                    operand(fa[t & 1][i]), operand(fb[t & 1][j]), acc[i][j], kFp4, kFp4, t, sa[0][i], t, sb[0][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    for (int64_t s = 0; s < stages; ++s) {
+        depth(std::integral_constant<int, 0>{}, s);
+        depth(std::integral_constant<int, 1>{}, s);
+        depth(std::integral_constant<int, 2>{}, s);
+        sync();  // stage s has been read whole, stage s + 1 has arrived
+        next = codes_of(s + 2);
+        load_scales((s + 1) / kBatch + 1, static_cast<int>((s + 1) % kBatch) % kScaleLoads);
+        read_scales(s + 1, sa[1], sb[1]);
+        depth(std::integral_constant<int, 3>{}, s);
+        keep_scales(s + 1, sa[1], sb[1]);
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+            sa[0][i] = sa[1][i];
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+            sb[0][j] = sb[1][j];
+    }
+    // Out through LDS, 32 rows of the wave's columns at a time, so that a lane
+    // stores four columns.  Rows are kPitch floats apart: the two halves of a
+    // wave, four rows apart, then write different banks.
+    constexpr int kCols = 32 * FN, kPitch = kCols + 8, kLanes = kCols / 4;
+    static_assert(W * 32 * kPitch * 4 <= sizeof(smem) && kPitch % 16 == 8, "the waves' parts fit the stages");
+    sync();
+    float* mine = reinterpret_cast<float*>(smem) + wave * 32 * kPitch;
+    const int64_t col = col0 + wn * kCols + (lane % kLanes) * 4;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                mine[((r & 3) + 8 * (r >> 2) + 4 * half) * kPitch + 32 * j + (lane & 31)] = acc[i][j][r];
+        __builtin_amdgcn_wave_barrier();
+        const int64_t first = row0 + wm * 32 * FM + 32 * i;
+#pragma unroll
+        for (int r = 0; r < 32; r += 64 / kLanes) {
+            const int row = r + lane / kLanes;
+            const f32x4 v = *reinterpret_cast<const f32x4*>(mine + row * kPitch + (lane % kLanes) * 4);
+            if (first + row < g.m)
+                store_four<T>(out, (first + row) * g.ldo, col, g.n, v, g.accumulate != 0);
+        }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
-}  // namespace
-
-size_t mx4_matmul_workspace_bytes(int64_t, int64_t, int64_t)
+// out = the parts' sum, in their order (+ out): one thread per four columns.
+template <int T>
+__global__ __launch_bounds__(kBlock) void k_mx4_join(const float* parts, int32_t count, int64_t m, int64_t n,
+                                                     int64_t ldp, void* out, int64_t ldo, int32_t accumulate,
+                                                     uint32_t row0, uint32_t units, RowDiv div)
 {
-    return 256;
+    const uint32_t u = blockIdx.x * kBlock + threadIdx.x;
+    if (u >= units)
+        return;
+    const uint32_t in = div_row(u, div);
+    const int64_t row = row0 + in, col = int64_t(u - in * div.n) * 4;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int32_t c = 0; c < count; ++c)
+        v += *reinterpret_cast<const f32x4*>(parts + (c * m + row) * ldp + col);
+    store_four<T>(out, row * ldo, col, n, v, accumulate != 0);
 }
 
-hipError_t launch_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* as, int64_t ldas, const uint8_t* b,
-                             int64_t ldb, const uint8_t* bs, int64_t ldbs, int64_t m, int64_t n, int64_t k,
-                             int32_t type, void* out, int64_t ldo, int32_t accumulate, void*, hipStream_t stream)
+// ---------------------------------------------------------------------------
+// Few rows of a: every row of b is read once, straight into registers.
+// ---------------------------------------------------------------------------
+// A block forms 16 MT x 16 NT outputs; its waves share k in chunks of 16
+// blocks (512 elements), and add their sums through LDS in the waves' order.
+// Lane l holds row l % 16 of a fragment and, for instruction t = 0..3 of a
+// chunk, its block 4 t + l / 16: an instruction's load then covers 64
+// contiguous bytes of each row, a chunk's four 256.
+constexpr int kChunk = 16;
+
+template <int N>
+struct Fragments {
+    i32x4 v[N][4];
+    u32x4 s[N];
+
+    template <bool WHOLE>
+    __device__ __forceinline__ void load(const uint8_t* const (&p)[N], const uint8_t* const (&ps)[N], int64_t chunk,
+                                         int64_t nkb, int q)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            s[i] = *reinterpret_cast<const u32x4*>(ps[i] + chunk * kChunk);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const int64_t kb = chunk * kChunk + 4 * t + q;
+                if (WHOLE || kb < nkb)
+                    v[i][t] = *reinterpret_cast<const i32x4*>(p[i] + kb * kMxBlockBytes);
+                else
+                    v[i][t] = i32x4{0, 0, 0, 0};
+            }
+        }
+    }
+    // The scale byte of this lane's block in instruction t; of blocks past the
+    // last (their codes are 0) not a NaN's.
+    template <bool WHOLE>
+    __device__ __forceinline__ uint32_t scale(int i, int t, int64_t chunk, int64_t nkb, int q) const
+    {
+        const uint32_t b = s[i][t] >> (8 * q);
+        return WHOLE || chunk * kChunk + 4 * t + q < nkb ? b : 0u;
+    }
+};
+
+constexpr int kRowWaves = 8;
+
+template <int T, int MT, int NT>
+__global__ __launch_bounds__(64 * kRowWaves) void k_mx4_rows_by(MatmulArgs g)
 {
-    if (m == 0 || n == 0)
-        return hipSuccess;
-    const int64_t tiles_n = (n + 63) / 64, tiles = (m + 63) / 64 * tiles_n, nkb = (k + 31) / 32;
+    __shared__ f32x4 part[kRowWaves][MT][NT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
+    const int waves = blockDim.x >> 6;
+    const int block = g.first + blockIdx.x, tm = block % g.tiles_m, tn = block / g.tiles_m;
+    const int64_t row0 = int64_t(tm) * 16 * MT, col0 = int64_t(tn) * 16 * NT;
+    const uint8_t *pa[MT], *sa[MT], *pb[NT], *sb[NT];
+    // rows past the end are read as the last one; what they give is not stored
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t r = row0 + 16 * i + (lane & 15) < g.m ? row0 + 16 * i + (lane & 15) : g.m - 1;
+        pa[i] = g.a + r * g.lda;
+        sa[i] = g.as + r * g.ldas;
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int64_t r = col0 + 16 * j + (lane & 15) < g.n ? col0 + 16 * j + (lane & 15) : g.n - 1;
+        pb[j] = g.b + r * g.ldb;
+        sb[j] = g.bs + r * g.ldbs;
+    }
+    f32x4 acc[MT][NT] = {};
+    const int64_t nkb = g.nkb, chunks = (nkb + kChunk - 1) / kChunk, whole = nkb / kChunk;
+    const auto multiply = [&](auto all, const Fragments<MT>& fa, const Fragments<NT>& fb, int64_t c) {
+        constexpr bool W = decltype(all)::value;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const uint32_t s = fb.template scale<W>(j, t, c, nkb, q);
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                        operand(fa.v[i][t]), operand(fb.v[j][t]), acc[i][j], kFp4, kFp4, 0,
+                        fa.template scale<W>(i, t, c, nkb, q), 0, s);
+            }
+    };
+    int64_t c = wave;
+    for (; c + waves < whole; c += 2 * waves) {  // two chunks' loads at a time
+        Fragments<NT> b0, b1;
+        Fragments<MT> a0, a1;
+        b0.template load<true>(pb, sb, c, nkb, q);
+        b1.template load<true>(pb, sb, c + waves, nkb, q);
+        a0.template load<true>(pa, sa, c, nkb, q);
+        a1.template load<true>(pa, sa, c + waves, nkb, q);
+        multiply(std::true_type{}, a0, b0, c);
+        multiply(std::true_type{}, a1, b1, c + waves);
+    }
+    for (; c < chunks; c += waves) {
+        Fragments<NT> b0;
+        Fragments<MT> a0;
+        b0.template load<false>(pb, sb, c, nkb, q);
+        a0.template load<false>(pa, sa, c, nkb, q);
+        multiply(std::false_type{}, a0, b0, c);
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+            part[wave][i][j][lane] = acc[i][j];
+    __syncthreads();
+    for (int f = wave; f < MT * NT; f += waves) {
+        const int i = f / NT, j = f % NT;
+        f32x4 v = part[0][i][j][lane];
+        for (int w = 1; w < waves; ++w)
+            v += part[w][i][j][lane];
+        const int64_t col = col0 + 16 * j + (lane & 15);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int64_t row = row0 + 16 * i + 4 * q + r;
+            if (row < g.m && col < g.n)
+                store_out<T>(g.out, row * g.ldo + col, v[r], g.accumulate != 0);
+        }
+    }
+}
+
+// `blocks` blocks of `threads`, in launches of at most the cap.
+template <typename F>
+hipError_t over_blocks(F kernel, MatmulArgs g, int64_t blocks, unsigned threads, hipStream_t stream)
+{
     const int64_t cap = one_shot_cap();
-    for (int64_t t = 0; t < tiles; t += cap) {
-        const unsigned grid = static_cast<unsigned>(tiles - t < cap ? tiles - t : cap);
-        const auto f = type == kF32 ? k_mx4_matmul<kF32> : type == kBF16 ? k_mx4_matmul<kBF16> : k_mx4_matmul<kF16>;
-        f<<<grid, kBlock, 0, stream>>>(a, lda, as, ldas, b, ldb, bs, ldbs, m, n, nkb, out, ldo, accumulate, t,
-                                       tiles_n);
+    for (int64_t b = 0; b < blocks; b += cap) {
+        g.first = static_cast<int32_t>(b);
+        kernel<<<static_cast<unsigned>(blocks - b < cap ? blocks - b : cap), threads, 0, stream>>>(g);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess)
             return e;
     }
     return hipSuccess;
+}
+
+template <int T, int WM, int WN, int FM, int FN>
+hipError_t tiles(MatmulArgs g, int32_t parts, float* ws, hipStream_t stream)
+{
+    constexpr int BM = 32 * WM * FM, BN = 32 * WN * FN;
+    g.tiles_m = static_cast<int32_t>((g.m + BM - 1) / BM);
+    g.tiles_n = static_cast<int32_t>((g.n + BN - 1) / BN);
+    if (parts == 1) {
+        g.part_blocks = g.nkb;
+        g.part_bytes = 0;
+        return over_blocks(k_mx4_tiles<T, WM, WN, FM, FN>, g, int64_t(g.tiles_m) * g.tiles_n, 64 * WM * WN, stream);
+    }
+    constexpr int64_t kUnit = kBatch * kStageBlocks;
+    MatmulArgs p = g;
+    p.part_blocks = ((g.nkb + kUnit - 1) / kUnit + parts - 1) / parts * kUnit;
+    p.ldo = (g.n + 3) / 4 * 4;
+    p.part_bytes = g.m * p.ldo * 4;
+    p.out = ws;
+    p.accumulate = 0;
+    hipError_t e = over_blocks(k_mx4_tiles<kF32, WM, WN, FM, FN>, p, int64_t(g.tiles_m) * g.tiles_n * parts,
+                               64 * WM * WN, stream);
+    const int64_t per_row = p.ldo / 4, most = (int64_t(1) << 30) / per_row < 1 ? 1 : (int64_t(1) << 30) / per_row;
+    const RowDiv div = row_div(static_cast<uint32_t>(per_row));
+    for (int64_t r = 0; r < g.m && e == hipSuccess; r += most) {
+        const uint32_t units = static_cast<uint32_t>((g.m - r < most ? g.m - r : most) * per_row);
+        k_mx4_join<T><<<(units + kBlock - 1) / kBlock, kBlock, 0, stream>>>(
+            ws, parts, g.m, g.n, p.ldo, g.out, g.ldo, g.accumulate, static_cast<uint32_t>(r), units, div);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+template <int T, int MT, int NT>
+hipError_t rows_by(MatmulArgs g, hipStream_t stream)
+{
+    g.tiles_m = static_cast<int32_t>((g.m + 16 * MT - 1) / (16 * MT));
+    g.tiles_n = static_cast<int32_t>((g.n + 16 * NT - 1) / (16 * NT));
+    const int64_t chunks = (g.nkb + kChunk - 1) / kChunk;
+    const unsigned waves = chunks < 1 ? 1u : chunks < kRowWaves ? static_cast<unsigned>(chunks) : kRowWaves;
+    return over_blocks(k_mx4_rows_by<T, MT, NT>, g, int64_t(g.tiles_m) * g.tiles_n, 64 * waves, stream);
+}
+
+template <int T>
+hipError_t product(const MatmulArgs& g, const MatmulPlan& plan, float* ws, hipStream_t stream)
+{
+    switch (plan.form) {
+    case MatmulPlan::kRows1: return rows_by<T, 1, 1>(g, stream);
+    case MatmulPlan::kRows2: return rows_by<T, 2, 2>(g, stream);
+    case MatmulPlan::kRows4: return rows_by<T, 4, 2>(g, stream);
+    case MatmulPlan::kTiles128: return tiles<T, 2, 2, 2, 2>(g, plan.parts, ws, stream);
+    default: return tiles<T, 2, 4, 4, 2>(g, plan.parts, ws, stream);
+    }
+}
+
+}  // namespace
+
+size_t mx4_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k)
+{
+    const MatmulPlan plan = matmul_plan(m, n, k);
+    return plan.parts > 1 ? align256(static_cast<size_t>(plan.parts) * m * ((n + 3) / 4 * 4) * sizeof(float)) : 256;
+}
+
+hipError_t launch_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* as, int64_t ldas, const uint8_t* b,
+                             int64_t ldb, const uint8_t* bs, int64_t ldbs, int64_t m, int64_t n, int64_t k,
+                             int32_t type, void* out, int64_t ldo, int32_t accumulate, void* ws, hipStream_t stream)
+{
+    if (m == 0 || n == 0)
+        return hipSuccess;
+    constexpr int64_t kMostLd = 1 << 23;  // a tile's rows lie within a buffer's 2^31 bytes
+    MatmulPlan plan = matmul_plan(m, n, k);
+    const MatmulArgs g = {a, as, b, bs, lda, ldas, ldb, ldbs, m, n, (k + 31) / 32, out, ldo, accumulate, 0, 0, 0, 0, 0};
+    if (plan.form >= MatmulPlan::kTiles128 && (lda > kMostLd || ldb > kMostLd || ldas > kMostLd || ldbs > kMostLd))
+        plan = {MatmulPlan::kRows4, 1};
+    const auto f = type == kF32 ? product<kF32> : type == kBF16 ? product<kBF16> : product<kF16>;
+    return f(g, plan, static_cast<float*>(ws), stream);
 }
 
 }  // namespace uq

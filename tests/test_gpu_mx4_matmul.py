@@ -63,7 +63,7 @@ def case(m, n, k, dtype, accumulate, seed, lo=126, hi=128, pad=1):
 
 SHAPES = [(1, 1, 1), (1, 8, 32), (1, 64, 33), (1, 1000, 4096), (2, 17, 100), (3, 300, 31), (8, 129, 4000), (16, 64, 64),
           (17, 33, 2047), (31, 32, 512), (33, 1025, 96), (64, 64, 128), (65, 127, 1024), (100, 500, 255), (128, 128, 256),
-          (129, 260, 257), (255, 256, 4096), (256, 256, 32), (257, 513, 320), (300, 1, 700), (512, 768, 1000), (1100, 40, 64)]
+          (129, 260, 257), (255, 256, 4096), (256, 256, 32), (257, 513, 320), (300, 1, 700), (512, 768, 1000), (1100, 40, 64), (3300, 2900, 520)]
 
 
 @pytest.mark.parametrize("m,n,k", SHAPES)
