@@ -12,6 +12,7 @@ namespace {
 typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
+constexpr int kFp4 = 4;    // the matrix instructions' operand format
 constexpr int kBatch = 4;  // stages of 256 along k whose scale bytes a tile loads together
 
 // Which form a product takes; it goes by the sizes alone, and so does the
