@@ -52,21 +52,32 @@ __device__ __forceinline__ void load_octet(const void* row, int64_t col, int64_t
     }
 }
 
-// Eight stochastic fields of row `worker`, octet `oct`.
-__device__ __forceinline__ uint32_t mx4_stochastic(const float (&x)[8], uint32_t byte, uint64_t oct, uint32_t worker,
-                                                   uint64_t seed)
+// Eight stochastic fields of row `row`, octet `oct`, from the complement of
+// the block of their words' high halves; the low halves' block is formed only
+// where the high ones leave one of the eight undecided (once in 4096).
+__device__ __forceinline__ uint32_t mx4_stochastic(const float (&x)[8], uint32_t byte, const uint4& halves,
+                                                   uint32_t oct, uint32_t row, uint64_t seed)
 {
-    const float to_half = mx4_half_units(byte);
-    const uint32_t k0 = static_cast<uint32_t>(seed), k1 = static_cast<uint32_t>(seed >> 32);
-    const uint32_t c0 = static_cast<uint32_t>(oct), c1 = static_cast<uint32_t>(oct >> 32);
-    const uint4 hi = philox4x32_10(c0, c1, worker, 0, k0, k1), lo = philox4x32_10(c0, c1, worker, 1, k0, k1);
-    uint32_t w = 0;
+    const Mx4Place place = mx4_places(byte);
+    const uint32_t w[4] = {halves.x, halves.y, halves.z, halves.w};
+    uint32_t sum[8], least = ~0u;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t r = (philox_half(hi, j) << 16) | philox_half(lo, j);
-        w |= (mx4_exact(x[j], to_half, r) | (__float_as_uint(x[j]) >> 31 << 3)) << (4 * j);
+    for (int j = 0; j < 4; ++j) {
+        sum[j] = mx4_carry<0>(x[j], place, w[j]);
+        sum[4 + j] = mx4_carry<1>(x[4 + j], place, w[j]);
+        const uint32_t a = mx4_undecided(sum[j]), b = mx4_undecided(sum[4 + j]);
+        const uint32_t c = a < b ? a : b;
+        least = least < c ? least : c;
     }
-    return w;
+    if (least < kUndecided || byte >= kMxTop) {
+        const uint4 lo = philox4x32_10(oct, 0, row, 1, static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t hi = ~(j < 4 ? w[j & 3] << 16 : w[j & 3]) & 0xFFFF0000u;
+            sum[j] = mx4_exact(x[j], mx4_half_units(byte), hi | philox_half(lo, j)) << 24;
+        }
+    }
+    return mx4_pack(sum, x);
 }
 
 // Codes along the rows: one thread per octet, the four threads of a block's
@@ -84,103 +95,223 @@ __global__ __launch_bounds__(kBlock) void k_mx4_rows(const void* x, int64_t cols
     const uint32_t row = row0 + in;
     float v[8];
     load_octet<T>(static_cast<const char*>(x) + row * ldx * kElemBytes<T>, int64_t(oct) * 8, cols, v);
+    uint4 halves;
+    if constexpr (SR) {
+        const uint32_t k0 = static_cast<uint32_t>(seed), k1 = static_cast<uint32_t>(seed >> 32);
+        halves = philox_tail_not(row_key(0, row, k0), lane_key(oct, 0, k1), k0, k1);
+    }
     const uint32_t byte = mx4_byte(quad_max(octet_max(v)));
-    uint32_t w = SR ? mx4_stochastic(v, byte, oct, row, seed) : mx4_nearest(v, byte);
+    uint32_t w;
+    if constexpr (SR)
+        w = mx4_stochastic(v, byte, halves, oct, row, seed);
+    else
+        w = mx4_nearest(v, byte);
     w = byte == kMxNaN ? 0u : w;
     *reinterpret_cast<uint32_t*>(codes + row * ldc + int64_t(oct) * 4) = w;
     if ((oct & 3) == 0)
         scales[row * lds + oct / 4] = static_cast<uint8_t>(byte);
 }
 
-// Codes of the transposed matrix: one thread per column and block of 32 rows.
-template <int T, bool SR>
-__global__ __launch_bounds__(kBlock) void k_mx4_cols(const void* x, int64_t rows, int64_t cols, int64_t ldx,
-                                                     uint64_t seed, uint8_t* codes, int64_t ldc, uint8_t* scales,
-                                                     int64_t lds, int64_t unit0, int64_t units, int64_t col_units)
+// Codes of the transposed matrix, and with ROWS of the rows too, from one
+// read: a block takes 128 rows by 64 columns through LDS.  A thread first
+// holds octets of four rows (32 apart, the same columns, so that their Philox
+// blocks share the lane's part), forms the rows' codes from them and leaves
+// the elements in LDS together with the complements of their words' high
+// halves; then a thread takes 32 rows of one column, a whole block.  Four
+// lanes take a column's four blocks, 64 contiguous bytes of its codes.
+// Columns are turned by 16 every 32 rows: those four lanes then read
+// different banks.
+constexpr int kTileRows = 128, kTileCols = 64;
+
+__device__ __forceinline__ int tile_at(int row, int col)
 {
-    const int64_t u = unit0 + int64_t(blockIdx.x) * kBlock + threadIdx.x;
-    if (u >= units)
+    return row * kTileCols + ((col + 16 * (row >> 5)) & (kTileCols - 1));
+}
+
+// Block -> tile.  Blocks go to the eight XCDs in turn, and each XCD has its own
+// L2: eight blocks that one XCD takes in a row cover 2 tiles down and 4 across,
+// so that the 128-byte lines which they write in part, two blocks' codes of a
+// column and four blocks' codes of a row, leave it whole (8192 x 8192 bf16
+// to the nearest, both ways: 37.1 us, 42.4 with the tiles of a column
+// in turn).
+constexpr int kSuperDown = 2, kSuperAcross = 4, kSuper = kSuperDown * kSuperAcross, kXcds = 8;
+
+__host__ __device__ __forceinline__ int64_t super_blocks(int64_t down, int64_t across)
+{
+    const int64_t all = ((down + kSuperDown - 1) / kSuperDown) * ((across + kSuperAcross - 1) / kSuperAcross);
+    return (all + kXcds - 1) / kXcds * kXcds * kSuper;
+}
+__device__ __forceinline__ bool place_tile(int64_t block, int32_t down, int32_t across, int64_t* tr, int64_t* tc)
+{
+    const int64_t turn = block / kXcds, super = turn / kSuper * kXcds + block % kXcds;
+    const int in = static_cast<int>(turn % kSuper), per_row = (across + kSuperAcross - 1) / kSuperAcross;
+    const int64_t row = super / per_row;
+    *tr = row * kSuperDown + in / kSuperAcross;
+    *tc = (super - row * per_row) * kSuperAcross + in % kSuperAcross;
+    return *tr < down && *tc < across;
+}
+
+template <int T, bool SR, bool ROWS>
+__global__ __launch_bounds__(kBlock) void k_mx4_tiles(const void* x, int64_t rows, int64_t cols, int64_t ldx,
+                                                      uint64_t seed, uint8_t* codes, int64_t ldc, uint8_t* scales,
+                                                      int64_t lds, uint8_t* codes_t, int64_t ldct, uint8_t* scales_t,
+                                                      int64_t ldst, int64_t first, int32_t down, int32_t across)
+{
+    // 16-bit types: half | element << 16; binary32: the halves apart
+    __shared__ __attribute__((aligned(16))) uint32_t elems[kTileRows * kTileCols];
+    __shared__ __attribute__((aligned(16))) uint16_t apart[T == kF32 && SR ? kTileRows * kTileCols : 1];
+    int64_t tr, tc;
+    if (!place_tile(first + blockIdx.x, down, across, &tr, &tc))
         return;
-    const int64_t blk = u / col_units, col = u - blk * col_units;
-    if (col >= cols)
-        return;
-    float v[4][8];
-    uint32_t top = 0;
+    const int64_t row0 = tr * kTileRows, col0 = tc * kTileCols;
+    const uint32_t k0 = static_cast<uint32_t>(seed), k1 = static_cast<uint32_t>(seed >> 32);
+    {
+        const int oc = threadIdx.x & 7, r0 = threadIdx.x >> 3;
+        const uint32_t oct = static_cast<uint32_t>(col0 / 8) + oc;
+        float v[4][8];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-        const int64_t row = blk * 32 + j;
-        float t = 0.0f;
-        if (row < rows) {
-            if constexpr (T == kF32)
-                t = static_cast<const float*>(x)[row * ldx + col];
-            else if constexpr (T == kBF16)
-                t = __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(x)[row * ldx + col]) << 16);
-            else
-                t = static_cast<float>(static_cast<const _Float16*>(x)[row * ldx + col]);
+        for (int i = 0; i < 4; ++i) {
+            const int64_t row = row0 + r0 + 32 * i;
+            load_octet<T>(static_cast<const char*>(x) + row * ldx * kElemBytes<T>, int64_t(oct) * 8,
+                          row < rows ? cols : 0, v[i]);
         }
-        v[j / 8][j % 8] = t;
-        const uint32_t b = __float_as_uint(t) & 0x7FFFFFFFu;
-        top = top > b ? top : b;
-    }
-    const uint32_t byte = mx4_byte(top);
-    u32x4 w;
-    for (int q = 0; q < 4; ++q) {
-        if constexpr (SR) {
-            const float to_half = mx4_half_units(byte);
-            const uint32_t k0 = static_cast<uint32_t>(seed), k1 = static_cast<uint32_t>(seed >> 32);
-            const uint32_t c0 = static_cast<uint32_t>(col / 8), c1 = static_cast<uint32_t>((col / 8) >> 32);
-            uint32_t f = 0;
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t row = static_cast<uint32_t>(blk * 32 + q * 8 + j);
-                const uint4 hi = philox4x32_10(c0, c1, row, 0, k0, k1), lo = philox4x32_10(c0, c1, row, 1, k0, k1);
-                const uint32_t r = (philox_half(hi, col & 7) << 16) | philox_half(lo, col & 7);
-                f |= (mx4_exact(v[q][j], to_half, r) | (__float_as_uint(v[q][j]) >> 31 << 3)) << (4 * j);
+        LaneKey lk;
+        if constexpr (SR)
+            lk = lane_key(oct, 0, k1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = r0 + 32 * i;
+            const uint32_t row = static_cast<uint32_t>(row0 + r);
+            uint4 halves = make_uint4(0, 0, 0, 0);
+            if constexpr (SR)
+                halves = philox_tail_not(row_key(0, row, k0), lk, k0, k1);
+            if constexpr (ROWS) {
+                const uint32_t byte = mx4_byte(quad_max(octet_max(v[i])));
+                uint32_t w;
+                if constexpr (SR)
+                    w = mx4_stochastic(v[i], byte, halves, oct, row, seed);
+                else
+                    w = mx4_nearest(v[i], byte);
+                if (row < rows && (oct & ~3u) * 8 < cols) {
+                    *reinterpret_cast<uint32_t*>(codes + row * ldc + int64_t(oct) * 4) = byte == kMxNaN ? 0u : w;
+                    if ((oct & 3) == 0)
+                        scales[row * lds + oct / 4] = static_cast<uint8_t>(byte);
+                }
             }
-            w[q] = f;
+            const uint32_t h[4] = {halves.x, halves.y, halves.z, halves.w};
+            const int at = tile_at(r, oc * 8);
+            uint32_t d[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                uint32_t e = __float_as_uint(v[i][j]);
+                if constexpr (T == kF16) {
+                    const _Float16 f = static_cast<_Float16>(v[i][j]);
+                    e = static_cast<uint32_t>(__builtin_bit_cast(uint16_t, f)) << 16;
+                }
+                if constexpr (T != kF32 && SR)  // bytes 2, 3 of the element, 0, 1 or 2, 3 of the word
+                    e = __builtin_amdgcn_perm(e, h[j & 3], j < 4 ? 0x07060100u : 0x07060302u);
+                d[j] = e;
+            }
+            *reinterpret_cast<u32x4*>(elems + at) = u32x4{d[0], d[1], d[2], d[3]};
+            *reinterpret_cast<u32x4*>(elems + at + 4) = u32x4{d[4], d[5], d[6], d[7]};
+            if constexpr (T == kF32 && SR)
+                *reinterpret_cast<u32x4*>(apart + at) =
+                    u32x4{(h[0] & 0xFFFFu) | h[1] << 16, (h[2] & 0xFFFFu) | h[3] << 16, h[0] >> 16 | (h[1] & 0xFFFF0000u),
+                          h[2] >> 16 | (h[3] & 0xFFFF0000u)};
+        }
+    }
+    __syncthreads();
+    const int q = threadIdx.x & 3, c = threadIdx.x >> 2;
+    const int64_t col = col0 + c, blk = row0 / kMxBlock + q;
+    if (col >= cols || blk * kMxBlock >= rows)
+        return;
+    const auto value = [](uint32_t d) {
+        if constexpr (T == kF16) {
+            const uint16_t e = static_cast<uint16_t>(d >> 16);
+            return static_cast<float>(__builtin_bit_cast(_Float16, e));
         } else {
-            w[q] = mx4_nearest(v[q], byte);
+            return __uint_as_float(T == kF32 || !SR ? d : d & 0xFFFF0000u);
+        }
+    };
+    uint32_t d[4][8], top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            d[i][j] = elems[tile_at(32 * q + 8 * i + j, c)];
+            // bf16: the largest has the largest upper half, whatever lies below
+            v[j] = T == kF16 ? value(d[i][j]) : __uint_as_float(d[i][j]);
+        }
+        top = octet_max(v, top);
+    }
+    if constexpr (T == kBF16 && SR)
+        top &= 0xFFFF0000u;
+    const uint32_t byte = mx4_byte(top);
+    scales_t[col * ldst + blk] = static_cast<uint8_t>(byte);
+    const Mx4Place place = mx4_places(byte);
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v[j] = value(d[i][j]);
+        if constexpr (SR) {
+            uint32_t sum[8], least = ~0u;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                sum[j] = mx4_carry<0>(v[j], place, T == kF32 ? apart[tile_at(32 * q + 8 * i + j, c)] : d[i][j]);
+                const uint32_t a = mx4_undecided(sum[j]);
+                least = least < a ? least : a;
+            }
+            w[i] = mx4_pack(sum, v);
+            if (least < kUndecided || byte >= kMxTop) {
+#pragma unroll 1
+                for (int j = 0; j < 8; ++j) {  // each element has a block of low halves of its own
+                    const int r = 32 * q + 8 * i + j, at = tile_at(r, c);
+                    const uint32_t e = elems[at];
+                    const uint4 lo = philox4x32_10(static_cast<uint32_t>(col >> 3), 0, static_cast<uint32_t>(row0) + r,
+                                                   1, k0, k1);
+                    const uint32_t hi = ~(T == kF32 ? apart[at] : e) << 16;
+                    const uint32_t code = mx4_exact(value(e), mx4_half_units(byte), hi | philox_half(lo, col & 7));
+                    w[i] = (w[i] & ~(7u << (4 * j))) | code << (4 * j);
+                }
+            }
+        } else {
+            w[i] = mx4_nearest(v, byte);
         }
     }
     if (byte == kMxNaN)
         w = u32x4{0, 0, 0, 0};
-    *reinterpret_cast<u32x4*>(codes + col * ldc + blk * kMxBlockBytes) = w;
-    scales[col * lds + blk] = static_cast<uint8_t>(byte);
+    *reinterpret_cast<u32x4*>(codes_t + col * ldct + blk * kMxBlockBytes) = w;
 }
 
-// One thread per octet: 4 bytes of codes and the block's byte in, eight
-// values out.  The converters decode, scale and round once, and give NaN for
-// the scale byte 255.
+// 16 bytes of values a thread (four in binary32, else eight): the codes of
+// those and the block's byte in.  The converters decode, scale and round
+// once, and give NaN for the scale byte 255.  Values leave nontemporally:
+// 16384 x 8192 bf16 47.4 us, 63.6 with plain stores; 4096^2 5.9 and 7.5.
 template <int T>
 __global__ __launch_bounds__(kBlock) void k_mx4_read(const uint8_t* codes, int64_t ldc, const uint8_t* scales,
                                                      int64_t lds, int64_t cols, void* out, int64_t ldo,
                                                      uint32_t row0, uint32_t units, RowDiv div)
 {
+    constexpr int kEach = 16 / kElemBytes<T>;
     const uint32_t u = blockIdx.x * kBlock + threadIdx.x;
     if (u >= units)
         return;
     const uint32_t in = div_row(u, div);
-    const uint32_t oct = u - in * div.n;
-    const uint32_t row = row0 + in;
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + row * ldc + int64_t(oct) * 4);
-    const float s = __uint_as_float(static_cast<uint32_t>(scales[row * lds + oct / 4]) << 23);
-    const int64_t col = int64_t(oct) * 8;
+    const uint32_t at = u - in * div.n;
+    const int64_t row = int64_t(row0) + in, col = int64_t(at) * kEach;
+    const float s = __uint_as_float(static_cast<uint32_t>(scales[row * lds + at / (kMxBlock / kEach)]) << 23);
+    const uint8_t* from = codes + row * ldc + int64_t(at) * (kEach / 2);
+    u32x4 v;
     if constexpr (T == kF32) {
-        const f32x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0),
-                            __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1),
-                            __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2),
-                            __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3)};
-        float* o = static_cast<float*>(out) + row * ldo + col;
-        if (col + 8 <= cols) {
-            reinterpret_cast<f32x4*>(o)[0] = f32x4{p[0][0], p[0][1], p[1][0], p[1][1]};
-            reinterpret_cast<f32x4*>(o)[1] = f32x4{p[2][0], p[2][1], p[3][0], p[3][1]};
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (col + j < cols)
-                    o[j] = p[j / 2][j % 2];
-        }
+        const uint32_t w = *reinterpret_cast<const uint16_t*>(from);
+        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
+        v = u32x4{__float_as_uint(a[0]), __float_as_uint(a[1]), __float_as_uint(b[0]), __float_as_uint(b[1])};
     } else {
-        u32x4 v;
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(from);
         if constexpr (T == kBF16) {
             v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
             v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
@@ -192,16 +323,20 @@ __global__ __launch_bounds__(kBlock) void k_mx4_read(const uint8_t* codes, int64
             v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 2));
             v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 3));
         }
-        uint16_t* o = static_cast<uint16_t*>(out) + row * ldo + col;
-        if (col + 8 <= cols) {
-            *reinterpret_cast<u32x4*>(o) = v;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (col + j < cols)
-                    o[j] = static_cast<uint16_t>(v[j / 2] >> (16 * (j % 2)));
-        }
     }
+    char* to = static_cast<char*>(out) + (row * ldo + col) * kElemBytes<T>;
+    if (col + kEach <= cols) {
+        __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(to));
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+        if (col + j < cols) {
+            if constexpr (T == kF32)
+                reinterpret_cast<uint32_t*>(to)[j] = v[j];
+            else
+                reinterpret_cast<uint16_t*>(to)[j] = static_cast<uint16_t>(v[j / 2] >> (16 * (j % 2)));
+        }
 }
 
 // Bytes shared by `rows` gradients (and, with accumulate, the bytes held):
@@ -218,8 +353,7 @@ __global__ __launch_bounds__(kBlock) void k_mx4_shared(const float* g, int64_t d
     for (int32_t m = 0; m < rows; ++m) {
         float v[8];
         load_octet<kF32>(g + m * ldg, o * 8, d, v);
-        const uint32_t t = octet_max(v);
-        top = top > t ? top : t;
+        top = octet_max(v, top);
     }
     uint32_t byte = mx4_byte(quad_max(top));
     if ((o & 3) == 0) {
@@ -317,41 +451,45 @@ hipError_t over_rows(int64_t rows, int64_t per_row, F launch)
     return hipSuccess;
 }
 
-template <int T>
-hipError_t quantise(const void* x, int64_t rows, int64_t cols, int64_t ldx, bool sr, uint64_t seed, uint8_t* codes,
-                    int64_t ldc, uint8_t* scales, int64_t lds, uint8_t* codes_t, int64_t ldct, uint8_t* scales_t,
-                    int64_t ldst, hipStream_t stream)
+struct QuantiseArgs {
+    const void* x;
+    int64_t rows, cols, ldx;
+    uint64_t seed;
+    uint8_t* codes;
+    int64_t ldc;
+    uint8_t* scales;
+    int64_t lds;
+    uint8_t* codes_t;
+    int64_t ldct;
+    uint8_t* scales_t;
+    int64_t ldst;
+};
+
+template <int T, bool SR>
+hipError_t quantise(const QuantiseArgs& a, hipStream_t stream)
 {
-    hipError_t e = hipSuccess;
-    if (codes != nullptr) {
-        const int64_t per_row = blocks_for(cols, kMxBlock) * 4;
+    if (a.codes_t == nullptr) {
+        const int64_t per_row = blocks_for(a.cols, kMxBlock) * 4;
         const RowDiv div = row_div(static_cast<uint32_t>(per_row));
-        e = over_rows(rows, per_row, [&](uint32_t row0, uint32_t units) {
-            const unsigned grid = static_cast<unsigned>(blocks_for(units, kBlock));
-            if (sr)
-                k_mx4_rows<T, true><<<grid, kBlock, 0, stream>>>(x, cols, ldx, seed, codes, ldc, scales, lds, row0,
-                                                                units, div);
-            else
-                k_mx4_rows<T, false><<<grid, kBlock, 0, stream>>>(x, cols, ldx, seed, codes, ldc, scales, lds, row0,
-                                                                 units, div);
+        return over_rows(a.rows, per_row, [&](uint32_t row0, uint32_t units) {
+            k_mx4_rows<T, SR><<<static_cast<unsigned>(blocks_for(units, kBlock)), kBlock, 0, stream>>>(
+                a.x, a.cols, a.ldx, a.seed, a.codes, a.ldc, a.scales, a.lds, row0, units, div);
         });
     }
-    if (e == hipSuccess && codes_t != nullptr) {
-        const int64_t col_units = blocks_for(cols, 64) * 64;
-        const int64_t units = blocks_for(rows, kMxBlock) * col_units;
-        const int64_t cap = one_shot_cap() * kBlock;
-        for (int64_t u = 0; u < units && e == hipSuccess; u += cap) {
-            const unsigned grid = static_cast<unsigned>(blocks_for(units - u < cap ? units - u : cap, kBlock));
-            if (sr)
-                k_mx4_cols<T, true><<<grid, kBlock, 0, stream>>>(x, rows, cols, ldx, seed, codes_t, ldct, scales_t,
-                                                                ldst, u, units, col_units);
-            else
-                k_mx4_cols<T, false><<<grid, kBlock, 0, stream>>>(x, rows, cols, ldx, seed, codes_t, ldct, scales_t,
-                                                                 ldst, u, units, col_units);
-            e = hipGetLastError();
-        }
+    const int32_t down = static_cast<int32_t>(blocks_for(a.rows, kTileRows));
+    const int32_t across = static_cast<int32_t>(blocks_for(a.cols, kTileCols));
+    const int64_t tiles = super_blocks(down, across);
+    const int64_t cap = one_shot_cap();
+    const auto kernel = a.codes != nullptr ? k_mx4_tiles<T, SR, true> : k_mx4_tiles<T, SR, false>;
+    for (int64_t t = 0; t < tiles; t += cap) {
+        kernel<<<static_cast<unsigned>(tiles - t < cap ? tiles - t : cap), kBlock, 0, stream>>>(
+            a.x, a.rows, a.cols, a.ldx, a.seed, a.codes, a.ldc, a.scales, a.lds, a.codes_t, a.ldct, a.scales_t, a.ldst,
+            t, down, across);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
     }
-    return e;
+    return hipSuccess;
 }
 
 }  // namespace
@@ -362,8 +500,12 @@ hipError_t launch_mx4_quantize(const void* x, int32_t type, int64_t rows, int64_
 {
     if (rows == 0 || cols == 0)
         return hipSuccess;
-    const auto f = type == kF32 ? quantise<kF32> : type == kBF16 ? quantise<kBF16> : quantise<kF16>;
-    return f(x, rows, cols, ldx, stochastic, seed, codes, ldc, scales, lds, codes_t, ldct, scales_t, ldst, stream);
+    const QuantiseArgs a = {x, rows, cols, ldx, seed, codes, ldc, scales, lds, codes_t, ldct, scales_t, ldst};
+    if (stochastic)
+        return type == kF32 ? quantise<kF32, true>(a, stream)
+                            : type == kBF16 ? quantise<kBF16, true>(a, stream) : quantise<kF16, true>(a, stream);
+    return type == kF32 ? quantise<kF32, false>(a, stream)
+                        : type == kBF16 ? quantise<kBF16, false>(a, stream) : quantise<kF16, false>(a, stream);
 }
 
 hipError_t launch_mx4_dequantize(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t rows,
@@ -371,7 +513,7 @@ hipError_t launch_mx4_dequantize(const uint8_t* codes, int64_t ldc, const uint8_
 {
     if (rows == 0 || cols == 0)
         return hipSuccess;
-    const int64_t per_row = blocks_for(cols, 8);
+    const int64_t per_row = blocks_for(cols, type == kF32 ? 4 : 8);
     const RowDiv div = row_div(static_cast<uint32_t>(per_row));
     return over_rows(rows, per_row, [&](uint32_t row0, uint32_t units) {
         const unsigned grid = static_cast<unsigned>(blocks_for(units, kBlock));

@@ -79,20 +79,22 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v)
     return v > b ? v : b;
 }
 
-__device__ __forceinline__ uint32_t max3_u32(uint32_t a, uint32_t b, uint32_t c)
+// The largest of |a|, |b| and |c| in one instruction; a NaN if one is.
+__device__ __forceinline__ float max3_abs(float a, float b, float c)
 {
-    const uint32_t m = a > b ? a : b;
-    return m > c ? m : c;
+    float r;
+    __asm__("v_maximum3_f32 %0, |%1|, |%2|, |%3|" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
 }
 
-// Bits of the largest |x| of eight.
-__device__ __forceinline__ uint32_t octet_max(const float (&x)[8])
+// Bits of the largest |x| of eight, and of `most`; at or above 0x7F800000 if
+// one of them is a NaN or an infinity.
+__device__ __forceinline__ uint32_t octet_max(const float (&x)[8], uint32_t most = 0)
 {
-    uint32_t m = 0;
-#pragma unroll
-    for (int j = 0; j < 8; j += 2)
-        m = max3_u32(m, __float_as_uint(x[j]) & 0x7FFFFFFFu, __float_as_uint(x[j + 1]) & 0x7FFFFFFFu);
-    return m;
+    float m = max3_abs(__uint_as_float(most), x[0], x[1]);
+    m = max3_abs(m, x[2], x[3]);
+    m = max3_abs(m, x[4], x[5]);
+    return __float_as_uint(max3_abs(m, x[6], x[7]));
 }
 
 // Eight 4-bit fields to the nearest code, ties to the even one: the
@@ -126,6 +128,64 @@ __device__ __forceinline__ uint32_t mx4_exact(float x, float to_half, uint32_t r
     const float l = floorf(q);
     const uint32_t t = static_cast<uint32_t>((q - l) * 4294967296.0f);
     return static_cast<uint32_t>(l) + (sb >> 22) - 256u + (r < t ? 1u : 0u);
+}
+
+// The stochastic code of one element from the high half of its uniform word,
+// without the division into steps: with y = |x| in half units, m = y + max(y, 2)
+// is the code's place in binary32, for its bits 22 and up are 256 plus the code
+// (y < 2: 2 + y has the codes 0 and 1 a half apart; beyond, 2 y keeps one bit
+// below the leading one) and the 22 bits below are the fraction.  m is formed
+// in x's own units, |x| + max(|x|, 2^e), and the power of two between them
+// added to its exponent.  Adding the complement of the high half on the
+// fraction's upper 16 bits carries into the code exactly when the half is
+// below them.  What is returned is the sum shifted up by two: the code is its
+// top byte.  The sum's fraction tells where that decided wrongly
+// (mx4_undecided): the halves were equal, or m, which rounds where y < 2,
+// carried into the fraction's upper 16 bits.  From byte kMxTop on m may pass
+// the largest binary32; those blocks are decided by whole words alone.
+constexpr uint32_t kMxTop = 252;
+struct Mx4Place {
+    float least;      // 2^e
+    uint32_t to_half; // what to add to m's bits, shifted by two as they are
+};
+__device__ __forceinline__ Mx4Place mx4_places(uint32_t byte)
+{
+    return {__uint_as_float(byte << 23), (128u - byte) << 25};
+}
+// `halves`: a word of the complement; HALF picks the 16 bits.
+template <int HALF>
+__device__ __forceinline__ uint32_t mx4_carry(float x, Mx4Place p, uint32_t halves)
+{
+    // One instruction each: fmaxf would first make x canonical, and the
+    // compiler takes the sum with a shifted byte apart.
+    float m;
+    uint32_t place, r;
+    __asm__("v_max_f32 %0, |%1|, %2" : "=v"(m) : "v"(x), "v"(p.least));
+    m += fabsf(x);
+    __asm__("v_lshl_add_u32 %0, %1, 2, %2" : "=v"(place) : "v"(m), "v"(p.to_half));
+    if constexpr (HALF == 0)
+        __asm__("v_mad_u32_u16 %0, %1, %2, %3" : "=v"(r) : "v"(halves), "s"(256), "v"(place));
+    else
+        __asm__("v_mad_u32_u16 %0, %1, %2, %3 op_sel:[1,0,0,0]" : "=v"(r) : "v"(halves), "s"(256), "v"(place));
+    return r;
+}
+// Below kUndecided where the fraction of a sum lies within 64 of a carry.
+constexpr uint32_t kUndecided = 128u << 10;
+__device__ __forceinline__ uint32_t mx4_undecided(uint32_t sum)
+{
+    return (sum + 256u) << 8;
+}
+
+// Fields from eight sums (codes in their top bytes) and the elements' signs.
+__device__ __forceinline__ uint32_t mx4_pack(const uint32_t (&sum)[8], const float (&x)[8])
+{
+    const auto tops = [](uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+        return __builtin_amdgcn_perm(b, a, 0x0C0C0703u) | __builtin_amdgcn_perm(d, c, 0x07030C0Cu);
+    };
+    const uint32_t even = tops(sum[0], sum[2], sum[4], sum[6]), odd = tops(sum[1], sum[3], sum[5], sum[7]);
+    const uint32_t se = tops(__float_as_uint(x[0]), __float_as_uint(x[2]), __float_as_uint(x[4]), __float_as_uint(x[6]));
+    const uint32_t so = tops(__float_as_uint(x[1]), __float_as_uint(x[3]), __float_as_uint(x[5]), __float_as_uint(x[7]));
+    return (even | odd << 4) | ((se >> 4) & 0x08080808u) | (so & 0x80808080u);
 }
 
 // |code| in half units.
