@@ -52,15 +52,16 @@ __device__ __forceinline__ void load_octet(const void* row, int64_t col, int64_t
     }
 }
 
-// Eight stochastic fields of row `row`, octet `oct`, from the complement of
-// the block of their words' high halves; the low halves' block is formed only
-// where the high ones leave one of the eight undecided (once in 4096).
-__device__ __forceinline__ uint32_t mx4_stochastic(const float (&x)[8], uint32_t byte, const uint4& halves,
-                                                   uint32_t oct, uint32_t row, uint64_t seed)
+// Eight stochastic codes of row `row`, octet `oct`, in the top bytes of sum,
+// from the complement of the block of their words' high halves; the low
+// halves' block is formed only where the high ones leave one of the eight
+// undecided (once in 4096).
+__device__ __forceinline__ void mx4_codes(const float (&x)[8], uint32_t byte, const uint4& halves, uint64_t oct,
+                                          uint32_t row, uint64_t seed, uint32_t (&sum)[8])
 {
     const Mx4Place place = mx4_places(byte);
     const uint32_t w[4] = {halves.x, halves.y, halves.z, halves.w};
-    uint32_t sum[8], least = ~0u;
+    uint32_t least = ~0u;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         sum[j] = mx4_carry<0>(x[j], place, w[j]);
@@ -70,13 +71,22 @@ __device__ __forceinline__ uint32_t mx4_stochastic(const float (&x)[8], uint32_t
         least = least < c ? least : c;
     }
     if (least < kUndecided || byte >= kMxTop) {
-        const uint4 lo = philox4x32_10(oct, 0, row, 1, static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32));
+        const uint4 lo = philox4x32_10(static_cast<uint32_t>(oct), static_cast<uint32_t>(oct >> 32), row, 1,
+                                       static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32));
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const uint32_t hi = ~(j < 4 ? w[j & 3] << 16 : w[j & 3]) & 0xFFFF0000u;
             sum[j] = mx4_exact(x[j], mx4_half_units(byte), hi | philox_half(lo, j)) << 24;
         }
     }
+}
+
+// The same as eight fields.
+__device__ __forceinline__ uint32_t mx4_stochastic(const float (&x)[8], uint32_t byte, const uint4& halves,
+                                                   uint32_t oct, uint32_t row, uint64_t seed)
+{
+    uint32_t sum[8];
+    mx4_codes(x, byte, halves, oct, row, seed, sum);
     return mx4_pack(sum, x);
 }
 
@@ -374,60 +384,150 @@ __device__ __forceinline__ float mx4_mean_factor(uint32_t byte, float inv_m)
     return byte == kMxNaN ? __uint_as_float(0x7FC00000u) : half * inv_m;
 }
 
-// The rows' codes in half units on the given bytes, added into sum, and with
-// out the mean.  FORM: the bytes are formed from the rows first and stored.
-template <bool FORM>
+// Eight results of each lane, stored: a wave's 512 coordinates from `first` on.
+// Lanes 32 apart exchange a half of theirs, so that each of the two stores
+// covers 1 KiB without gaps (16 bytes a lane 32 bytes apart took twice the
+// time as nontemporal stores).
+template <bool NT, typename V>
+__device__ __forceinline__ void store_octets(V* to, int64_t first, int64_t d, int lane, const uint32_t (&r)[8])
+{
+    if (first + 512 <= d) {
+        u32x4 a, b;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const u32x2 p = __builtin_amdgcn_permlane32_swap(r[j], r[4 + j], false, false);
+            a[j] = p[0];  // coordinates j of octet lane, or 4 + j of octet lane - 32
+            b[j] = p[1];  // coordinates j of octet lane + 32, or 4 + j of octet lane
+        }
+        uint32_t* o = reinterpret_cast<uint32_t*>(to) + first + (lane & 31) * 8 + (lane >> 5) * 4;
+        if constexpr (NT) {
+            __builtin_nontemporal_store(a, reinterpret_cast<u32x4*>(o));
+            __builtin_nontemporal_store(b, reinterpret_cast<u32x4*>(o + 256));
+        } else {
+            reinterpret_cast<u32x4*>(o)[0] = a;
+            reinterpret_cast<u32x4*>(o + 256)[0] = b;
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (first + lane * 8 + j < d)
+            reinterpret_cast<uint32_t*>(to)[first + lane * 8 + j] = r[j];
+}
+
+// The mean (with out) of the sums and their stores.
+template <bool NT>
+__device__ __forceinline__ void finish_octet(const int32_t (&total)[8], uint32_t byte, float inv_m, int64_t first,
+                                             int64_t d, int lane, int32_t* sum, float* out)
+{
+    uint32_t r[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        r[j] = static_cast<uint32_t>(total[j]);
+    store_octets<NT>(sum, first, d, lane, r);
+    if (out == nullptr)
+        return;
+    const float deq = mx4_mean_factor(byte, inv_m);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        r[j] = __float_as_uint(static_cast<float>(total[j]) * deq);
+    store_octets<NT>(out, first, d, lane, r);
+}
+
+// The whole step for up to ROWS rows: a lane holds its octet of every row in
+// registers, so each gradient is read once.  A wave takes 512 coordinates.
+template <int ROWS, bool NT>
+__global__ __launch_bounds__(kBlock) void k_mx4_step(const float* g, int64_t d, int32_t rows, int64_t ldg,
+                                                     uint64_t seed, uint8_t* scales, int32_t* sum, float inv_m,
+                                                     float* out, int64_t oct0, int64_t octs)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t o = oct0 + int64_t(blockIdx.x) * kBlock + threadIdx.x;
+    float v[ROWS][8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int m = 0; m < ROWS; ++m)
+        if (m < rows)
+            load_octet<kF32>(g + m * ldg, o * 8, d, v[m]);
+#pragma unroll
+    for (int m = 0; m < ROWS; ++m)
+        if (m < rows)
+            top = octet_max(v[m], top);
+    const uint32_t byte = mx4_byte(quad_max(top));
+    if ((o & 3) == 0 && o < octs)
+        scales[o / 4] = static_cast<uint8_t>(byte);
+    const uint32_t k0 = static_cast<uint32_t>(seed), k1 = static_cast<uint32_t>(seed >> 32);
+    const LaneKey lk = lane_key(static_cast<uint32_t>(o), 0, k1);
+    // the counter's high word is the same in the whole block: 2^32 is a multiple of its octets
+    const uint32_t high = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(o >> 32));
+    int32_t total[8] = {};
+#pragma unroll
+    for (int from = 0; from < ROWS; from += kMxByteRows) {
+        Mx4Bytes bytes;
+#pragma unroll
+        for (int m = from; m < from + kMxByteRows && m < ROWS; ++m)
+            if (m < rows) {
+                uint32_t codes[8];
+                mx4_codes(v[m], byte, philox_tail_not(row_key(high, m, k0), lk, k0, k1), o, m, seed, codes);
+                bytes.add(codes, v[m]);
+            }
+        const int held = rows - from < 0 ? 0 : rows - from < kMxByteRows ? rows - from : kMxByteRows;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            total[j] += bytes.total(j, held);
+    }
+    if (byte == kMxNaN) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            total[j] = 0;
+    }
+    finish_octet<NT>(total, byte, inv_m, (o - lane) * 8, d, lane, sum, out);
+}
+
+// The rows' codes on given bytes, added into sum (= or +=), and with out the mean.
+template <bool NT>
 __global__ __launch_bounds__(kBlock) void k_mx4_sum(const float* g, int64_t d, int32_t rows, int64_t ldg,
-                                                    int32_t worker0, uint8_t* scales, uint64_t seed,
+                                                    int32_t worker0, const uint8_t* scales, uint64_t seed,
                                                     int32_t accumulate, int32_t* sum, float inv_m, float* out,
                                                     int64_t oct0, int64_t octs)
 {
+    const int lane = threadIdx.x & 63;
     const int64_t o = oct0 + int64_t(blockIdx.x) * kBlock + threadIdx.x;
-    if (o >= octs)
-        return;
-    uint32_t byte;
-    if constexpr (FORM) {
-        uint32_t top = 0;
-        for (int32_t m = 0; m < rows; ++m) {
-            float v[8];
-            load_octet<kF32>(g + m * ldg, o * 8, d, v);
-            const uint32_t t = octet_max(v);
-            top = top > t ? top : t;
-        }
-        byte = mx4_byte(quad_max(top));
-        if ((o & 3) == 0)
-            scales[o / 4] = static_cast<uint8_t>(byte);
-    } else {
-        byte = scales[o / 4];
+    uint32_t byte = o < octs ? scales[o / 4] : 1u;
+    byte = byte > 1u ? byte : 1u;
+    int32_t total[8] = {};
+    if (accumulate) {
+        float held[8];
+        load_octet<kF32>(sum, o * 8, d, held);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            total[j] = __float_as_int(held[j]);
     }
-    const float to_half = mx4_half_units(byte);
-    int32_t acc[8] = {};
     const uint32_t k0 = static_cast<uint32_t>(seed), k1 = static_cast<uint32_t>(seed >> 32);
-    const uint32_t c0 = static_cast<uint32_t>(o), c1 = static_cast<uint32_t>(o >> 32);
-    if (byte != kMxNaN)
-        for (int32_t m = 0; m < rows; ++m) {
+    const LaneKey lk = lane_key(static_cast<uint32_t>(o), 0, k1);
+    const uint32_t high = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(o >> 32));
+    const float most = __uint_as_float(byte << 23) * 6.0f;
+    for (int32_t from = 0; from < rows; from += kMxByteRows) {
+        Mx4Bytes bytes;
+        const int held = rows - from < kMxByteRows ? rows - from : kMxByteRows;
+        for (int m = 0; m < held; ++m) {
             float v[8];
-            load_octet<kF32>(g + m * ldg, o * 8, d, v);
-            const uint32_t id = static_cast<uint32_t>(worker0 + m);
-            const uint4 hi = philox4x32_10(c0, c1, id, 0, k0, k1), lo = philox4x32_10(c0, c1, id, 1, k0, k1);
+            load_octet<kF32>(g + (from + m) * ldg, o * 8, d, v);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t r = (philox_half(hi, j) << 16) | philox_half(lo, j);
-                const int32_t h = mx4_half_value(mx4_exact(v[j], to_half, r));
-                acc[j] += v[j] < 0.0f ? -h : h;
-            }
+            for (int j = 0; j < 8; ++j)  // the byte may not be this row's: no more than the largest code
+                v[j] = copysignf(fminf(fabsf(v[j]), most), v[j]);
+            uint32_t codes[8];
+            const uint32_t id = static_cast<uint32_t>(worker0 + from + m);
+            mx4_codes(v, byte, philox_tail_not(row_key(high, id, k0), lk, k0, k1), o, id, seed, codes);
+            bytes.add(codes, v);
         }
-    const float deq = mx4_mean_factor(byte, inv_m);
+        if (byte != kMxNaN) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int64_t i = o * 8 + j;
-        if (i < d) {
-            const int32_t s = acc[j] + (accumulate ? sum[i] : 0);
-            sum[i] = s;
-            if (out != nullptr)
-                out[i] = static_cast<float>(s) * deq;
+            for (int j = 0; j < 8; ++j)
+                total[j] += bytes.total(j, held);
         }
     }
+    finish_octet<NT>(total, byte, inv_m, (o - lane) * 8, d, lane, sum, out);
 }
 
 int64_t blocks_for(int64_t units, int64_t per)
@@ -548,23 +648,35 @@ hipError_t launch_mx4_shared_scale(const float* g, int64_t d, int32_t rows, int6
     });
 }
 
+// Sums and outputs beyond this many bytes of each leave nontemporally.
+constexpr int64_t kMxNontemporalBytes = int64_t(46) << 20;
+
 hipError_t launch_mx4_quantize_sum(const float* g, int64_t d, int32_t rows, int64_t ldg, int32_t worker0,
                                    const uint8_t* scales, uint64_t seed, int32_t accumulate, int32_t* sum, int32_t M,
                                    float* out, hipStream_t stream)
 {
     const float inv_m = out != nullptr ? 1.0f / static_cast<float>(M) : 0.0f;
+    const auto kernel = 4 * d > kMxNontemporalBytes ? k_mx4_sum<true> : k_mx4_sum<false>;
     return over_octets(d, [&](int64_t o, int64_t octs, unsigned grid) {
-        k_mx4_sum<false><<<grid, kBlock, 0, stream>>>(g, d, rows, ldg, worker0, const_cast<uint8_t*>(scales), seed,
-                                                      accumulate, sum, inv_m, out, o, octs);
+        kernel<<<grid, kBlock, 0, stream>>>(g, d, rows, ldg, worker0, scales, seed, accumulate, sum, inv_m, out, o,
+                                            octs);
     });
+}
+
+template <bool NT>
+static auto step_kernel(int32_t rows)
+{
+    return rows <= 2 ? k_mx4_step<2, NT> : rows <= 4 ? k_mx4_step<4, NT> : rows <= 8 ? k_mx4_step<8, NT>
+                                                                                     : k_mx4_step<16, NT>;
 }
 
 hipError_t launch_mx4_aggregate(const float* g, int64_t d, int32_t M, int64_t ldg, uint64_t seed, uint8_t* scales,
                                 int32_t* sum, float* out, hipStream_t stream)
 {
     const float inv_m = 1.0f / static_cast<float>(M);
+    const auto kernel = 4 * d > kMxNontemporalBytes ? step_kernel<true>(M) : step_kernel<false>(M);
     return over_octets(d, [&](int64_t o, int64_t octs, unsigned grid) {
-        k_mx4_sum<true><<<grid, kBlock, 0, stream>>>(g, d, M, ldg, 0, scales, seed, 0, sum, inv_m, out, o, octs);
+        kernel<<<grid, kBlock, 0, stream>>>(g, d, M, ldg, seed, scales, sum, inv_m, out, o, octs);
     });
 }
 

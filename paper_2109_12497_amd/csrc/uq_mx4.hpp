@@ -152,7 +152,8 @@ __device__ __forceinline__ Mx4Place mx4_places(uint32_t byte)
 {
     return {__uint_as_float(byte << 23), (128u - byte) << 25};
 }
-// `halves`: a word of the complement; HALF picks the 16 bits.
+// `halves`: a word of the complement; HALF picks the 16 bits.  x as it is: at
+// most 6 * 2^e.
 template <int HALF>
 __device__ __forceinline__ uint32_t mx4_carry(float x, Mx4Place p, uint32_t halves)
 {
@@ -176,23 +177,55 @@ __device__ __forceinline__ uint32_t mx4_undecided(uint32_t sum)
     return (sum + 256u) << 8;
 }
 
+// The top bytes of four words.
+__device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    return __builtin_amdgcn_perm(b, a, 0x0C0C0703u) | __builtin_amdgcn_perm(d, c, 0x07030C0Cu);
+}
+
 // Fields from eight sums (codes in their top bytes) and the elements' signs.
 __device__ __forceinline__ uint32_t mx4_pack(const uint32_t (&sum)[8], const float (&x)[8])
 {
-    const auto tops = [](uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-        return __builtin_amdgcn_perm(b, a, 0x0C0C0703u) | __builtin_amdgcn_perm(d, c, 0x07030C0Cu);
-    };
-    const uint32_t even = tops(sum[0], sum[2], sum[4], sum[6]), odd = tops(sum[1], sum[3], sum[5], sum[7]);
-    const uint32_t se = tops(__float_as_uint(x[0]), __float_as_uint(x[2]), __float_as_uint(x[4]), __float_as_uint(x[6]));
-    const uint32_t so = tops(__float_as_uint(x[1]), __float_as_uint(x[3]), __float_as_uint(x[5]), __float_as_uint(x[7]));
+    const auto bits = [&](int j) { return __float_as_uint(x[j]); };
+    const uint32_t even = top_bytes(sum[0], sum[2], sum[4], sum[6]), odd = top_bytes(sum[1], sum[3], sum[5], sum[7]);
+    const uint32_t se = top_bytes(bits(0), bits(2), bits(4), bits(6)), so = top_bytes(bits(1), bits(3), bits(5), bits(7));
     return (even | odd << 4) | ((se >> 4) & 0x08080808u) | (so & 0x80808080u);
 }
 
-// |code| in half units.
-__device__ __forceinline__ int32_t mx4_half_value(uint32_t code)
-{
-    return code < 2u ? static_cast<int32_t>(code) : static_cast<int32_t>((2u | (code & 1u)) << ((code >> 1) - 1u));
-}
+// Sums over rows of eight signed codes in half units, biased by 12 a row and
+// held as bytes (even and odd elements apart): at most 24 a row, so up to
+// kMxByteRows rows.  A byte permutation looks a code's value up for four
+// elements at a time, in one table for each sign.
+constexpr int kMxByteRows = 8;
+struct Mx4Bytes {
+    uint32_t even = 0, odd = 0;
+
+    __device__ __forceinline__ void add(const uint32_t (&sum)[8], const float (&x)[8])
+    {
+        const auto bits = [&](int j) { return __float_as_uint(x[j]); };
+        even += values(top_bytes(sum[0], sum[2], sum[4], sum[6]), signs(bits(0), bits(2), bits(4), bits(6)));
+        odd += values(top_bytes(sum[1], sum[3], sum[5], sum[7]), signs(bits(1), bits(3), bits(5), bits(7)));
+    }
+    // The sum of element j over `rows` rows.
+    __device__ __forceinline__ int32_t total(int j, int rows) const
+    {
+        const uint32_t w = j & 1 ? odd : even;
+        return static_cast<int32_t>((w >> (8 * (j >> 1))) & 0xFFu) - 12 * rows;
+    }
+
+  private:
+    // 0xFF in the byte of a word whose top bit is set
+    static __device__ __forceinline__ uint32_t signs(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+    {
+        return __builtin_amdgcn_perm(b, a, 0x0C0C0B09u) | __builtin_amdgcn_perm(d, c, 0x0B090C0Cu);
+    }
+    static __device__ __forceinline__ uint32_t values(uint32_t codes, uint32_t negative)
+    {
+        const uint32_t plus = __builtin_amdgcn_perm(0x18141210u, 0x0F0E0D0Cu, codes);   // 24 20 18 16 15 14 13 12
+        const uint32_t minus = __builtin_amdgcn_perm(0x00040608u, 0x090A0B0Cu, codes);  // 0 4 6 8 9 10 11 12
+        return (plus & ~negative) | (minus & negative);
+    }
+};
 
 // Half h of a Philox block's words (uq.h: bits 16*(h / 4) .. +15 of word h mod 4).
 __device__ __forceinline__ uint32_t philox_half(const uint4& w, int h)
