@@ -115,7 +115,12 @@ def _stream(stream):
     if stream is None:
         import torch
 
-        return torch.cuda.current_stream().cuda_stream
+        # the raw handle of torch's current stream, without the Stream object
+        # that torch.cuda.current_stream() makes (0.25 us, 2.9 with it)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is None or not torch.cuda.is_initialized():
+            return torch.cuda.current_stream().cuda_stream
+        return raw(torch._C._cuda_getDevice())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

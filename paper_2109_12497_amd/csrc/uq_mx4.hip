@@ -9,13 +9,14 @@ namespace {
 // Elements 8 * octet .. + 7 of one row as binary32 (zeros past cols).  Whole
 // octets are read in 16-byte pieces (rows start on 16-byte boundaries), the
 // last ragged one element by element: nothing past cols is read.
-template <int T>
+template <int T, bool NT = false>
 __device__ __forceinline__ void load_octet(const void* row, int64_t col, int64_t cols, float (&x)[8])
 {
     if (col + 8 <= cols) {
         if constexpr (T == kF32) {
-            const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(row) + col);
-            const f32x4 a = p[0], b = p[1];
+            const float* p = static_cast<const float*>(row) + col;
+            const f32x4 a = NT ? load_nt(p) : *reinterpret_cast<const f32x4*>(p);
+            const f32x4 b = NT ? load_nt(p + 4) : *reinterpret_cast<const f32x4*>(p + 4);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 x[j] = a[j];
@@ -436,7 +437,8 @@ __device__ __forceinline__ void finish_octet(const int32_t (&total)[8], uint32_t
 
 // The whole step for up to ROWS rows: a lane holds its octet of every row in
 // registers, so each gradient is read once.  A wave takes 512 coordinates.
-template <int ROWS, bool NT>
+// LOADS: gradients read nontemporally.
+template <int ROWS, bool NT, bool LOADS>
 __global__ __launch_bounds__(kBlock) void k_mx4_step(const float* g, int64_t d, int32_t rows, int64_t ldg,
                                                      uint64_t seed, uint8_t* scales, int32_t* sum, float inv_m,
                                                      float* out, int64_t oct0, int64_t octs)
@@ -448,7 +450,7 @@ __global__ __launch_bounds__(kBlock) void k_mx4_step(const float* g, int64_t d, 
 #pragma unroll
     for (int m = 0; m < ROWS; ++m)
         if (m < rows)
-            load_octet<kF32>(g + m * ldg, o * 8, d, v[m]);
+            load_octet<kF32, LOADS>(g + m * ldg, o * 8, d, v[m]);
 #pragma unroll
     for (int m = 0; m < ROWS; ++m)
         if (m < rows)
@@ -482,6 +484,73 @@ __global__ __launch_bounds__(kBlock) void k_mx4_step(const float* g, int64_t d, 
             total[j] = 0;
     }
     finish_octet<NT>(total, byte, inv_m, (o - lane) * 8, d, lane, sum, out);
+}
+
+// The whole step with the rows of 512 coordinates spread over a block's four
+// waves (wave w takes w, w + 4, ...), which share their maxima and add their
+// sums through LDS.  1000 coordinates of 8 workers 3.4 us, 6.4 with a wave for
+// all rows.
+__global__ __launch_bounds__(kBlock) void k_mx4_step_spread(const float* g, int64_t d, int32_t rows, int64_t ldg,
+                                                         uint64_t seed, uint8_t* scales, int32_t* sum, float inv_m,
+                                                         float* out, int64_t oct0, int64_t octs)
+{
+    constexpr int kWaves = kBlock / 64, kEach = 16 / kWaves;
+    __shared__ uint32_t tops[kWaves][64];
+    __shared__ u32x2 sums[kWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t o = oct0 + int64_t(blockIdx.x) * 64 + lane;
+    float v[kEach][8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (wave + kWaves * i < rows)
+            load_octet<kF32>(g + (wave + kWaves * i) * ldg, o * 8, d, v[i]);
+    const uint32_t k0 = static_cast<uint32_t>(seed), k1 = static_cast<uint32_t>(seed >> 32);
+    const LaneKey lk = lane_key(static_cast<uint32_t>(o), 0, k1);
+    uint4 halves[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)  // while the rows arrive
+        halves[i] = philox_tail_not(row_key(static_cast<uint32_t>(o >> 32), wave + kWaves * i, k0), lk, k0, k1);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (wave + kWaves * i < rows)
+            top = octet_max(v[i], top);
+    tops[wave][lane] = top;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w)
+        top = top > tops[w][lane] ? top : tops[w][lane];
+    const uint32_t byte = mx4_byte(quad_max(top));
+    Mx4Bytes bytes;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (wave + kWaves * i < rows) {
+            uint32_t codes[8];
+            mx4_codes(v[i], byte, halves[i], o, wave + kWaves * i, seed, codes);
+            bytes.add(codes, v[i]);
+        }
+    sums[wave][lane] = u32x2{bytes.even, bytes.odd};
+    __syncthreads();
+    if (wave != 0)
+        return;
+    if ((o & 3) == 0 && o < octs)
+        scales[o / 4] = static_cast<uint8_t>(byte);
+    int32_t total[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        total[j] = bytes.total(j, rows);
+    for (int w = 1; w < kWaves; ++w) {
+        bytes.even = sums[w][lane][0];
+        bytes.odd = sums[w][lane][1];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            total[j] += bytes.total(j, 0);
+    }
+    if (byte == kMxNaN) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            total[j] = 0;
+    }
+    finish_octet<false>(total, byte, inv_m, (o - lane) * 8, d, lane, sum, out);
 }
 
 // The rows' codes on given bytes, added into sum (= or +=), and with out the mean.
@@ -626,13 +695,14 @@ hipError_t launch_mx4_dequantize(const uint8_t* codes, int64_t ldc, const uint8_
     });
 }
 
-// Octets of d coordinates, four to a block, in launches of at most the cap.
+// Octets of d coordinates, `each` to a block of threads, in launches of at
+// most the cap.
 template <typename F>
-static hipError_t over_octets(int64_t d, F launch)
+static hipError_t over_octets(int64_t d, int64_t each, F launch)
 {
-    const int64_t octs = blocks_for(d, kMxBlock) * 4, most = one_shot_cap() * kBlock;
+    const int64_t octs = blocks_for(d, kMxBlock) * 4, most = one_shot_cap() * each;
     for (int64_t o = 0; o < octs; o += most) {
-        launch(o, octs, static_cast<unsigned>(blocks_for(octs - o < most ? octs - o : most, kBlock)));
+        launch(o, octs, static_cast<unsigned>(blocks_for(octs - o < most ? octs - o : most, each)));
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess)
             return e;
@@ -643,7 +713,7 @@ static hipError_t over_octets(int64_t d, F launch)
 hipError_t launch_mx4_shared_scale(const float* g, int64_t d, int32_t rows, int64_t ldg, int32_t accumulate,
                                    uint8_t* scales, hipStream_t stream)
 {
-    return over_octets(d, [&](int64_t o, int64_t octs, unsigned grid) {
+    return over_octets(d, kBlock, [&](int64_t o, int64_t octs, unsigned grid) {
         k_mx4_shared<<<grid, kBlock, 0, stream>>>(g, d, rows, ldg, accumulate, scales, o, octs);
     });
 }
@@ -657,25 +727,38 @@ hipError_t launch_mx4_quantize_sum(const float* g, int64_t d, int32_t rows, int6
 {
     const float inv_m = out != nullptr ? 1.0f / static_cast<float>(M) : 0.0f;
     const auto kernel = 4 * d > kMxNontemporalBytes ? k_mx4_sum<true> : k_mx4_sum<false>;
-    return over_octets(d, [&](int64_t o, int64_t octs, unsigned grid) {
+    return over_octets(d, kBlock, [&](int64_t o, int64_t octs, unsigned grid) {
         kernel<<<grid, kBlock, 0, stream>>>(g, d, rows, ldg, worker0, scales, seed, accumulate, sum, inv_m, out, o,
                                             octs);
     });
 }
 
-template <bool NT>
+// Gradients beyond this many bytes, the Infinity Cache's size, are read
+// nontemporally: 8 workers of 25.6 M coordinates 176.6 us, 181.1 otherwise; 2 of
+// them (204 MB) 68.8 and 59.3.
+constexpr int64_t kMxStreamBytes = int64_t(256) << 20;
+// The rows are spread over a block's waves for 5 rows and more until the
+// outputs leave nontemporally, and for fewer up to this many coordinates: 8 rows
+// of 262,144 coordinates 4.2 us, 5.5 otherwise, of 11.2 M 80.3 and 85.4, of 25.6 M
+// 181.0 and 176.6; 2 rows of 262,144 3.0 either way, of 1.05 M 5.4 and 4.3.
+constexpr int64_t kMxSpread = int64_t(1) << 18;
+
+template <bool NT, bool LOADS>
 static auto step_kernel(int32_t rows)
 {
-    return rows <= 2 ? k_mx4_step<2, NT> : rows <= 4 ? k_mx4_step<4, NT> : rows <= 8 ? k_mx4_step<8, NT>
-                                                                                     : k_mx4_step<16, NT>;
+    return rows <= 2 ? k_mx4_step<2, NT, LOADS> : rows <= 4 ? k_mx4_step<4, NT, LOADS>
+         : rows <= 8 ? k_mx4_step<8, NT, LOADS> : k_mx4_step<16, NT, LOADS>;
 }
 
 hipError_t launch_mx4_aggregate(const float* g, int64_t d, int32_t M, int64_t ldg, uint64_t seed, uint8_t* scales,
                                 int32_t* sum, float* out, hipStream_t stream)
 {
     const float inv_m = 1.0f / static_cast<float>(M);
-    const auto kernel = 4 * d > kMxNontemporalBytes ? step_kernel<true>(M) : step_kernel<false>(M);
-    return over_octets(d, [&](int64_t o, int64_t octs, unsigned grid) {
+    const bool spread = 4 * d <= kMxNontemporalBytes && (M >= 5 || d <= kMxSpread);
+    const auto kernel = spread ? k_mx4_step_spread
+                      : 4 * d <= kMxNontemporalBytes ? step_kernel<false, false>(M)
+                      : 4 * d * M <= kMxStreamBytes ? step_kernel<true, false>(M) : step_kernel<true, true>(M);
+    return over_octets(d, spread ? 64 : kBlock, [&](int64_t o, int64_t octs, unsigned grid) {
         kernel<<<grid, kBlock, 0, stream>>>(g, d, M, ldg, seed, scales, sum, inv_m, out, o, octs);
     });
 }
