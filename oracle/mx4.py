@@ -41,7 +41,7 @@ def block_max(x: np.ndarray) -> np.ndarray:
     r, c = x.shape
     full = np.zeros((r, _blocks(c) * 32))
     full[:, :c] = np.abs(x.astype(np.float64))
-    return full.reshape(r, -1, 32).max(-1) if c else np.zeros((r, 0))
+    return full.reshape(r, _blocks(c), 32).max(-1)
 
 
 def bytes_of(top: np.ndarray) -> np.ndarray:
@@ -91,7 +91,7 @@ def quantize(x: np.ndarray, r: np.ndarray | None):
 
 def decode(codes: np.ndarray, scale_bytes: np.ndarray, cols: int) -> np.ndarray:
     """The values in 64 bits (NaN for byte 255)."""
-    f = np.stack([codes & 15, codes >> 4], axis=-1).reshape(codes.shape[0], -1)[:, :cols]
+    f = np.stack([codes & 15, codes >> 4], axis=-1).reshape(codes.shape[0], 2 * codes.shape[1])[:, :cols]
     v = np.where(f > 7, -1.0, 1.0) * LEVELS[f & 7]
     b = np.repeat(scale_bytes.astype(np.int64), 32, axis=1)[:, :cols]
     return np.where(b == 255, np.nan, v * 2.0 ** (np.where(b == 255, 0, b) - 127.0))

@@ -23,8 +23,13 @@ bounds the averaged iterate's suboptimality by
 which is the content of Theorems 2-3 for this problem.
 
 The aggregator is a callable (grads [M, ldg] fp32 device tensor, d, seed) ->
-[d] fp32 tensor.  `QuantisedAggregate` runs the library's four calls; the
-baseline is `mean_aggregate`.
+[d] fp32 tensor.  `QuantisedAggregate` runs the library's four calls,
+`Mx4Aggregate` the step on microscaled 4-bit codes; the baseline is
+`mean_aggregate`.
+
+The shard gradients are formed in binary64, or (`Mx4Gradients`) by a linear
+layer whose products run on 4-bit operands: A theta forward, A^T (A theta - b)
+backward.
 """
 from __future__ import annotations
 
@@ -33,7 +38,10 @@ from dataclasses import dataclass
 
 import torch
 
+from .mx4 import Mx4Linear, Mx4Step
 from .step import Step
+
+MX4 = "mx4"  # in place of a scale set: microscaled 4-bit codes
 
 
 @dataclass
@@ -97,9 +105,18 @@ def project(p: LeastSquares, theta: torch.Tensor) -> torch.Tensor:
 
 def variance_bound(p: LeastSquares, scales) -> float:
     """Lemma 1 / 2 excess second moment of one worker, averaged over M
-    independent workers; 0 for the unquantised mean (scales None)."""
+    independent workers; 0 for the unquantised mean (scales None).
+
+    On microscaled codes a coordinate between neighbours l and h of the grid
+    has variance (x - l)(h - x).  With 2^e < a / 3 for the block's shared
+    maximum a: at most (h - l)^2 / 4 <= 4^e <= a^2 / 9 anywhere; or at most
+    x^2 / 16 from 2^e on, where h - l <= |x| / 2, and |x| 2^e / 2 <= |x| a / 6
+    below.  Over the blocks, sum a^2 <= M W_max^2 and, by Cauchy-Schwarz twice,
+    sum |x| a <= sqrt(32 M) W_max^2."""
     if scales is None:
         return 0.0
+    if scales == MX4:
+        return min(32.0 / 9.0, (1.0 / 16.0 + math.sqrt(32.0 * p.M) / 6.0) / p.M) * p.W_max ** 2
     s_hat = float(min(scales))
     n = p.n
     return min(n / s_hat ** 2, math.sqrt(n) / s_hat) * p.W_max ** 2 / p.M
@@ -130,7 +147,44 @@ class QuantisedAggregate:
         return self.step.out[:d]
 
 
-def run_sgd(p: LeastSquares, aggregate, T: int, eta: float, seed: int, ldg: int | None = None) -> dict:
+class Mx4Aggregate:
+    """The library's aggregation on microscaled 4-bit codes."""
+
+    def __init__(self, d: int, M: int, device):
+        self.step = Mx4Step(d, M, device=device)
+
+    def __call__(self, grads: torch.Tensor, d: int, seed: int) -> torch.Tensor:
+        return self.step.run(grads, seed)
+
+
+class Mx4Gradients:
+    """shard_gradients through a layer of one output: y = A_m theta forward and
+    A_m^T (y - b_m) / rows backward, on 4-bit operands (theta and A_m rounded to
+    the nearest, the residuals stochastically)."""
+
+    def __init__(self, p: LeastSquares, seed: int = 0):
+        M, rows, n = p.A.shape
+        self.layer = Mx4Linear(rows, n, 1, device=p.A.device)
+        self.x = torch.zeros((M, rows, -(-n // 4) * 4), dtype=torch.float32, device=p.A.device)
+        self.x[:, :, :n].copy_(p.A)
+        self.seed = seed
+
+    def __call__(self, p: LeastSquares, theta: torch.Tensor, out: torch.Tensor) -> None:
+        n, rows = p.n, p.A.shape[1]
+        w = torch.zeros((1, -(-n // 4) * 4), dtype=torch.float32, device=theta.device)
+        w[0, :n].copy_(theta)
+        self.layer.load(w[:, :n])
+        dy = torch.zeros((rows, 4), dtype=torch.float32, device=theta.device)
+        for m in range(p.M):
+            y = self.layer.forward(self.x[m, :, :n])
+            dy[:, 0].copy_((y[:, 0].double() - p.b[m]) / rows)
+            self.seed += 1
+            _, dw = self.layer.backward(dy[:, :1], self.seed)
+            out[m, :n].copy_(dw[0])
+
+
+def run_sgd(p: LeastSquares, aggregate, T: int, eta: float, seed: int, ldg: int | None = None,
+            gradients=shard_gradients) -> dict:
     """T projected SGD steps from theta0 = 0.  Returns the suboptimality of
     the averaged iterate (1/T) sum_{t=1..T} theta_t (the quantity Theorems 1-3
     bound), of the last iterate, and of the mean of the last T/2 iterates."""
@@ -142,7 +196,7 @@ def run_sgd(p: LeastSquares, aggregate, T: int, eta: float, seed: int, ldg: int 
     avg = torch.zeros_like(theta)
     tail = torch.zeros_like(theta)
     for t in range(T):
-        shard_gradients(p, theta, grads)
+        gradients(p, theta, grads)
         g = aggregate(grads, n, seed * 1_000_003 + t).to(torch.float64)
         theta = project(p, theta - eta * g)
         avg += theta
@@ -165,7 +219,8 @@ CONFIGS = {
 }
 
 
-def convergence_table(p: LeastSquares, make_aggregate, T: int, seeds=(0, 1, 2), configs=None) -> dict:
+def convergence_table(p: LeastSquares, make_aggregate, T: int, seeds=(0, 1, 2), configs=None,
+                      gradients=shard_gradients) -> dict:
     """For every setting: the Theorem 1-3 bound and mean averaged-iterate gap
     at the theorem's step, and the mean tail gap at the common step 1/(2L).
     make_aggregate(scales) returns an aggregator (scales None: the mean)."""
@@ -175,8 +230,8 @@ def convergence_table(p: LeastSquares, make_aggregate, T: int, seeds=(0, 1, 2), 
         agg = make_aggregate(scales)
         sigma2 = variance_bound(p, scales)
         eta, bound = theorem_step(p, sigma2, T)
-        thm = [run_sgd(p, agg, T, eta, seed=s)["gap_avg"] for s in seeds]
-        fixed = [run_sgd(p, agg, T, 0.5 / p.L, seed=s)["gap_tail"] for s in seeds]
+        thm = [run_sgd(p, agg, T, eta, seed=s, gradients=gradients)["gap_avg"] for s in seeds]
+        fixed = [run_sgd(p, agg, T, 0.5 / p.L, seed=s, gradients=gradients)["gap_tail"] for s in seeds]
         table[name] = dict(sigma2_bound=sigma2, eta=eta, bound=bound, gap_avg=sum(thm) / len(thm),
                            gap_tail_fixed_step=sum(fixed) / len(fixed))
     return table
@@ -192,15 +247,20 @@ def main() -> int:
     ap.add_argument("--rows", type=int, default=4000)
     ap.add_argument("--T", type=int, default=300)
     ap.add_argument("--seed", type=int, default=1)
+    ap.add_argument("--gradients", choices=("exact", MX4), default="exact",
+                    help="shard gradients in binary64, or through 4-bit products")
     args = ap.parse_args()
     dev = torch.device("cuda", torch.cuda.current_device())
     p = make_problem(args.n, args.M, args.rows, args.seed, device=dev)
 
     def make(scales):
+        if scales == MX4:
+            return Mx4Aggregate(p.n, p.M, dev)
         return mean_aggregate if scales is None else QuantisedAggregate(p.n, p.M, scales, dev)
 
-    table = convergence_table(p, make, args.T)
-    print(json.dumps(dict(n=p.n, M=p.M, rows=args.rows, T=args.T, L=p.L, R=p.R, W_max=p.W_max, f_star=p.f_star,
+    gradients = Mx4Gradients(p, args.seed) if args.gradients == MX4 else shard_gradients
+    table = convergence_table(p, make, args.T, configs={**CONFIGS, MX4: MX4}, gradients=gradients)
+    print(json.dumps(dict(n=p.n, M=p.M, rows=args.rows, T=args.T, gradients=args.gradients, L=p.L, R=p.R, W_max=p.W_max, f_star=p.f_star,
                           table=table), indent=1))
     return 0
 
