@@ -18,8 +18,9 @@ constexpr int kBatch = 4;  // stages of 256 along k whose scale bytes a tile loa
 // Which form a product takes; it goes by the sizes alone, and so does the
 // order of its sums.
 struct MatmulPlan {
-    enum Form { kRows1, kRows2, kRows4, kTiles128, kTiles256 } form;
-    int32_t parts;  // of k, added afterwards (tiles)
+    enum Form { kRows, kTiles128, kTiles256 } form;
+    int32_t parts;   // of k, added afterwards (kTiles128)
+    int32_t mt, nt;  // 16 rows of a and of b that a block takes (kRows)
 };
 
 // Nanoseconds that tiles of 128 x 128 or 256 x 256 take, `stages` stages of 256
@@ -45,37 +46,52 @@ int64_t tiles_ns(int64_t m, int64_t n, int64_t stages, int64_t parts, bool large
     return parts > 1 ? ns + 6000 + m * n * 8 * parts / 6000 : ns;
 }
 
+// Few rows: a block reads mt fragments of a and nt of b.  What takes the time
+// is the loads that a compute unit issues, so the number of fragments that a
+// unit's blocks read decides: 37 x 10001 x 5003 9.4 us with nt = 4 (157 blocks),
+// 12.2 with 2 (313, two to a unit) and 11.7 with 1; 48 x 8192 x 8192 14.7 with
+// 2 (256 blocks), 20.1 and 20.9; 32 x 4096 x 4096 5.8 with 1, 7.0 with 2.
+MatmulPlan rows_plan(int64_t m, int64_t n)
+{
+    MatmulPlan best = {MatmulPlan::kRows, 1, m <= 16 ? 1 : m <= 32 ? 2 : m <= 48 ? 3 : 4, 1};
+    const int64_t down = (m + 16 * best.mt - 1) / (16 * best.mt), a = m < 16 * best.mt ? m : 16 * best.mt;
+    int64_t least = 0;
+    for (int32_t nt = 1; nt <= 4; nt *= 2) {
+        const int64_t blocks = down * ((n + 16 * nt - 1) / (16 * nt)), rows = (blocks + 255) / 256 * (a + 16 * nt);
+        if (nt == 1 || rows < least) {
+            least = rows;
+            best.nt = nt;
+        }
+    }
+    return best;
+}
+
 MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
 {
-    if (m <= 16 || k == 0)
-        return {MatmulPlan::kRows1, 1};
-    // 37 x 10001 x 5003 13.3 us in twos, 16.6 in ones
-    if (m <= 32)
-        return {MatmulPlan::kRows2, 1};
-    // 64 x 8192 x 8192 16.4 us in fours, 21.6 in ones, 26.4 in tiles
-    if (m <= 64)
-        return {MatmulPlan::kRows4, 1};
+    // 64 x 8192 x 8192 16.4 us as few rows, 26.4 in tiles
+    if (m <= 64 || k == 0)
+        return rows_plan(m, n);
     const int64_t stages = (k + 255) / 256, batches = (stages + kBatch - 1) / kBatch;
-    MatmulPlan best = {MatmulPlan::kTiles256, 1};
+    MatmulPlan best = {MatmulPlan::kTiles256, 1, 0, 0};
     int64_t least = tiles_ns(m, n, stages, 1, true);
     for (int32_t parts = 1; parts <= 8 && parts <= batches; parts *= 2) {
         const int64_t deep = parts == 1 ? stages : (batches + parts - 1) / parts * kBatch;
         const int64_t ns = tiles_ns(m, n, deep, parts, false);
         if (ns < least) {
             least = ns;
-            best = {MatmulPlan::kTiles128, parts};
+            best = {MatmulPlan::kTiles128, parts, 0, 0};
         }
     }
     return best;
 }
 
-template <int T>
-__device__ __forceinline__ void store_out(void* out, int64_t at, float v, bool accumulate)
+// The element at `at` of the output, of type `type` (the same for the whole launch).
+__device__ __forceinline__ void store_out(int32_t type, void* out, int64_t at, float v, bool accumulate)
 {
-    if constexpr (T == kF32) {
+    if (type == kF32) {
         float* o = static_cast<float*>(out) + at;
         *o = accumulate ? *o + v : v;
-    } else if constexpr (T == kBF16) {
+    } else if (type == kBF16) {
         __bf16* o = static_cast<__bf16*>(out) + at;
         *o = static_cast<__bf16>(accumulate ? static_cast<float>(*o) + v : v);
     } else {
@@ -92,7 +108,7 @@ __device__ __forceinline__ void store_four(void* out, int64_t row, int64_t col, 
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (col + j < n)
-                store_out<T>(out, row + col + j, v[j], accumulate);
+                store_out(T, out, row + col + j, v[j], accumulate);
         return;
     }
     if constexpr (T == kF32) {
@@ -164,7 +180,7 @@ struct MatmulArgs {
     int64_t m, n, nkb;
     void* out;
     int64_t ldo;
-    int32_t accumulate;
+    int32_t type, accumulate;
     int32_t tiles_m, tiles_n;
     int64_t part_blocks;  // blocks along k of a part (all of them: one part)
     int64_t part_bytes;   // between the parts' outputs
@@ -269,9 +285,12 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx4_tiles(MatmulArgs g)
         (__attribute__((address_space(3))) uint8_t*)smem));
     constexpr int kScalesAt = 2 * kStage;
 
-    const int tiles = g.tiles_m * g.tiles_n, block = g.first + blockIdx.x, part = block / tiles;
+    const int tiles = g.tiles_m * g.tiles_n, block = g.first + blockIdx.x, part = __builtin_amdgcn_readfirstlane(block / tiles);
     int tm, tn;
     place(block - part * tiles, g.tiles_m, g.tiles_n, &tm, &tn);
+    // the buffers' addresses have to be scalar for the loads that take them
+    tm = __builtin_amdgcn_readfirstlane(tm);
+    tn = __builtin_amdgcn_readfirstlane(tn);
     const int64_t kb0 = part * g.part_blocks;
     const int64_t nkb = g.nkb - kb0 < g.part_blocks ? g.nkb - kb0 : g.part_blocks;
     char* const out = static_cast<char*>(g.out) + part * g.part_bytes;
@@ -508,7 +527,7 @@ struct Fragments {
 
 constexpr int kRowWaves = 8;
 
-template <int T, int MT, int NT>
+template <int MT, int NT>
 __global__ __launch_bounds__(64 * kRowWaves) void k_mx4_rows_by(MatmulArgs g)
 {
     __shared__ f32x4 part[kRowWaves][MT][NT][64];
@@ -580,7 +599,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_mx4_rows_by(MatmulArgs g)
         for (int r = 0; r < 4; ++r) {
             const int64_t row = row0 + 16 * i + 4 * q + r;
             if (row < g.m && col < g.n)
-                store_out<T>(g.out, row * g.ldo + col, v[r], g.accumulate != 0);
+                store_out(g.type, g.out, row * g.ldo + col, v[r], g.accumulate != 0);
         }
     }
 }
@@ -631,25 +650,39 @@ hipError_t tiles(MatmulArgs g, int32_t parts, float* ws, hipStream_t stream)
     return e;
 }
 
-template <int T, int MT, int NT>
+template <int MT, int NT>
 hipError_t rows_by(MatmulArgs g, hipStream_t stream)
 {
     g.tiles_m = static_cast<int32_t>((g.m + 16 * MT - 1) / (16 * MT));
     g.tiles_n = static_cast<int32_t>((g.n + 16 * NT - 1) / (16 * NT));
     const int64_t chunks = (g.nkb + kChunk - 1) / kChunk;
     const unsigned waves = chunks < 1 ? 1u : chunks < kRowWaves ? static_cast<unsigned>(chunks) : kRowWaves;
-    return over_blocks(k_mx4_rows_by<T, MT, NT>, g, int64_t(g.tiles_m) * g.tiles_n, 64 * waves, stream);
+    return over_blocks(k_mx4_rows_by<MT, NT>, g, int64_t(g.tiles_m) * g.tiles_n, 64 * waves, stream);
+}
+
+template <int MT>
+hipError_t rows_by(const MatmulArgs& g, int32_t nt, hipStream_t stream)
+{
+    return nt == 1 ? rows_by<MT, 1>(g, stream) : nt == 2 ? rows_by<MT, 2>(g, stream) : rows_by<MT, 4>(g, stream);
 }
 
 template <int T>
+hipError_t tiles(const MatmulArgs& g, const MatmulPlan& plan, float* ws, hipStream_t stream)
+{
+    return plan.form == MatmulPlan::kTiles256 ? tiles<T, 2, 4, 4, 2>(g, 1, ws, stream)
+                                              : tiles<T, 2, 2, 2, 2>(g, plan.parts, ws, stream);
+}
+
 hipError_t product(const MatmulArgs& g, const MatmulPlan& plan, float* ws, hipStream_t stream)
 {
-    switch (plan.form) {
-    case MatmulPlan::kRows1: return rows_by<T, 1, 1>(g, stream);
-    case MatmulPlan::kRows2: return rows_by<T, 2, 2>(g, stream);
-    case MatmulPlan::kRows4: return rows_by<T, 4, 2>(g, stream);
-    case MatmulPlan::kTiles128: return tiles<T, 2, 2, 2, 2>(g, plan.parts, ws, stream);
-    default: return tiles<T, 2, 4, 4, 2>(g, plan.parts, ws, stream);
+    if (plan.form != MatmulPlan::kRows)
+        return g.type == kF32 ? tiles<kF32>(g, plan, ws, stream)
+                              : g.type == kBF16 ? tiles<kBF16>(g, plan, ws, stream) : tiles<kF16>(g, plan, ws, stream);
+    switch (plan.mt) {
+    case 1: return rows_by<1>(g, plan.nt, stream);
+    case 2: return rows_by<2>(g, plan.nt, stream);
+    case 3: return rows_by<3>(g, plan.nt, stream);
+    default: return rows_by<4>(g, plan.nt, stream);
     }
 }
 
@@ -669,11 +702,11 @@ hipError_t launch_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* as, i
         return hipSuccess;
     constexpr int64_t kMostLd = 1 << 23;  // a tile's rows lie within a buffer's 2^31 bytes
     MatmulPlan plan = matmul_plan(m, n, k);
-    const MatmulArgs g = {a, as, b, bs, lda, ldas, ldb, ldbs, m, n, (k + 31) / 32, out, ldo, accumulate, 0, 0, 0, 0, 0};
-    if (plan.form >= MatmulPlan::kTiles128 && (lda > kMostLd || ldb > kMostLd || ldas > kMostLd || ldbs > kMostLd))
-        plan = {MatmulPlan::kRows4, 1};
-    const auto f = type == kF32 ? product<kF32> : type == kBF16 ? product<kBF16> : product<kF16>;
-    return f(g, plan, static_cast<float*>(ws), stream);
+    const MatmulArgs g = {a, as, b, bs, lda, ldas, ldb, ldbs, m, n, (k + 31) / 32, out, ldo, type, accumulate,
+                          0, 0, 0, 0, 0};
+    if (plan.form != MatmulPlan::kRows && (lda > kMostLd || ldb > kMostLd || ldas > kMostLd || ldbs > kMostLd))
+        plan = rows_plan(m, n);
+    return product(g, plan, static_cast<float*>(ws), stream);
 }
 
 }  // namespace uq
