@@ -431,6 +431,7 @@ int uq_scatter_into(const float* vals, const uint32_t* sel, int64_t K, float* ou
  *   codes    [rows][ldc] bytes, ldc >= 16 * ceil(cols / 32), ldc % 16 == 0
  *   scales   [rows][lds] bytes, lds >= ceil(cols / 32), lds % 16 == 0
  * Both arrays hold whole rows of their leading dimension; 16-byte aligned.
+ * Leading dimensions of these and of matrices are below 2^36 bytes (UQ_ERANGE).
  * Calls that write them write 16 * ceil(cols / 32) bytes of a row's codes and
  * ceil(cols / 32) of its scales and leave the rest as it was, and what lies
  * there never enters a result.

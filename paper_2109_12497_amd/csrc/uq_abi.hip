@@ -636,13 +636,23 @@ int uq_scatter_into(const float* vals, const uint32_t* sel, int64_t K, float* ou
     return scatter(vals, sel, K, out, d, false, stream);
 }
 
+// Matrix kernels hold a row stride as 32 bits of 16-byte units.
+static int check_stride(int64_t bytes, const char* name)
+{
+    if (bytes >= int64_t(1) << 36)
+        return fail(UQ_ERANGE, "leading dimension of %s is 2^36 bytes or more", name);
+    return UQ_OK;
+}
+
 // The codes and scale bytes of a rows x cols matrix in 4-bit floating point.
 static int check_mx4(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t rows, int64_t cols,
                      const char* codes_name, const char* scales_name)
 {
     const int64_t blocks = rows > 0 ? (cols + 31) / 32 : 0;
     UQ_TRY(check_rows(codes, 16 * blocks, rows, ldc, 16, codes_name));
-    return check_rows(scales, blocks, rows, lds, 16, scales_name);
+    UQ_TRY(check_stride(ldc, codes_name));
+    UQ_TRY(check_rows(scales, blocks, rows, lds, 16, scales_name));
+    return check_stride(lds, scales_name);
 }
 
 static int check_extent(int64_t v, const char* name)
@@ -664,7 +674,8 @@ static int check_type(int32_t type)
 // A rows x cols matrix of `type`, rows on 16-byte boundaries.
 static int check_matrix(const void* p, int32_t type, int64_t rows, int64_t cols, int64_t ld, const char* name)
 {
-    return check_rows(p, rows > 0 ? cols : 0, rows, ld, type == UQ_F32 ? 4 : 8, name);
+    UQ_TRY(check_rows(p, rows > 0 ? cols : 0, rows, ld, type == UQ_F32 ? 4 : 8, name));
+    return check_stride(ld > kMaxElems / 4 ? kMaxElems : ld * (type == UQ_F32 ? 4 : 2), name);
 }
 
 int uq_mx4_quantize(const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ldx, int32_t stochastic,

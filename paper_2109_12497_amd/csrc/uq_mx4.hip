@@ -6,51 +6,73 @@
 namespace uq {
 namespace {
 
-// Elements 8 * octet .. + 7 of one row as binary32 (zeros past cols).  Whole
-// octets are read in 16-byte pieces (rows start on 16-byte boundaries), the
-// last ragged one element by element: nothing past cols is read.
+// Eight elements as they lie in memory.
+template <int T>
+struct Octet {
+    u32x4 part[T == kF32 ? 2 : 1];
+};
+
+// A whole octet in 16-byte pieces.
+template <int T, bool NT = false>
+__device__ __forceinline__ Octet<T> read_octet(const void* at)
+{
+    Octet<T> o;
+#pragma unroll
+    for (int i = 0; i < (T == kF32 ? 2 : 1); ++i)
+        o.part[i] = NT ? load_nt(static_cast<const uint32_t*>(at) + 4 * i) : static_cast<const u32x4*>(at)[i];
+    return o;
+}
+
+// The `left` first elements of an octet one by one, zeros past them.
+template <int T>
+__device__ __forceinline__ Octet<T> read_ragged(const void* at, int64_t left)
+{
+    Octet<T> o;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        uint32_t e = 0;
+        if constexpr (T == kF32) {
+            if (j < left)
+                e = static_cast<const uint32_t*>(at)[j];
+            o.part[j / 4][j % 4] = e;
+        } else {
+            if (j < left)
+                e = static_cast<const uint16_t*>(at)[j];
+            o.part[0][j / 2] = j % 2 ? o.part[0][j / 2] | e << 16 : e;
+        }
+    }
+    return o;
+}
+
+template <int T, bool NT = false>
+__device__ __forceinline__ Octet<T> read_some(const void* at, int64_t left)
+{
+    return left >= 8 ? read_octet<T, NT>(at) : read_ragged<T>(at, left);
+}
+
+template <int T>
+__device__ __forceinline__ void unpack_octet(const Octet<T>& o, float (&x)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if constexpr (T == kF32) {
+            x[j] = __uint_as_float(o.part[j / 4][j % 4]);
+        } else {
+            const uint32_t pair = o.part[0][j / 2];
+            if constexpr (T == kBF16)
+                x[j] = __uint_as_float(j % 2 ? pair & 0xFFFF0000u : pair << 16);
+            else
+                x[j] = static_cast<float>(__builtin_bit_cast(f16x2, pair)[j % 2]);
+        }
+    }
+}
+
+// Elements col .. col + 7 of one row as binary32 (zeros past cols; rows start
+// on 16-byte boundaries and nothing past cols is read).
 template <int T, bool NT = false>
 __device__ __forceinline__ void load_octet(const void* row, int64_t col, int64_t cols, float (&x)[8])
 {
-    if (col + 8 <= cols) {
-        if constexpr (T == kF32) {
-            const float* p = static_cast<const float*>(row) + col;
-            const f32x4 a = NT ? load_nt(p) : *reinterpret_cast<const f32x4*>(p);
-            const f32x4 b = NT ? load_nt(p + 4) : *reinterpret_cast<const f32x4*>(p + 4);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[j] = a[j];
-                x[4 + j] = b[j];
-            }
-        } else {
-            const u32x4 v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(row) + col);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (T == kBF16) {
-                    x[2 * j] = __uint_as_float(v[j] << 16);
-                    x[2 * j + 1] = __uint_as_float(v[j] & 0xFFFF0000u);
-                } else {
-                    const uint32_t pair = v[j];
-                    const f16x2 h = __builtin_bit_cast(f16x2, pair);
-                    x[2 * j] = static_cast<float>(h[0]);
-                    x[2 * j + 1] = static_cast<float>(h[1]);
-                }
-            }
-        }
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        x[j] = 0.0f;
-        if (col + j < cols) {
-            if constexpr (T == kF32)
-                x[j] = static_cast<const float*>(row)[col + j];
-            else if constexpr (T == kBF16)
-                x[j] = __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(row)[col + j]) << 16);
-            else
-                x[j] = static_cast<float>(static_cast<const _Float16*>(row)[col + j]);
-        }
-    }
+    unpack_octet<T>(read_some<T, NT>(static_cast<const char*>(row) + col * kElemBytes<T>, cols - col), x);
 }
 
 // Eight stochastic codes of row `row`, octet `oct`, in the top bytes of sum,
@@ -91,11 +113,18 @@ __device__ __forceinline__ uint32_t mx4_stochastic(const float (&x)[8], uint32_t
     return mx4_pack(sum, x);
 }
 
+// The start of row `row`: strides are multiples of 16 bytes, and in those
+// units one 32 x 32 -> 64 bit product forms the offset.
+__device__ __forceinline__ int64_t row_start(uint32_t row, uint32_t stride16)
+{
+    return static_cast<int64_t>((static_cast<uint64_t>(row) * stride16) << 4);
+}
+
 // Codes along the rows: one thread per octet, the four threads of a block's
 // octets share its maximum.  A unit of the grid is an octet of the padded rows.
 template <int T, bool SR>
-__global__ __launch_bounds__(kBlock) void k_mx4_rows(const void* x, int64_t cols, int64_t ldx, uint64_t seed,
-                                                     uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds,
+__global__ __launch_bounds__(kBlock) void k_mx4_rows(const void* x, int64_t cols, uint32_t ldx16, uint64_t seed,
+                                                     uint8_t* codes, uint32_t ldc16, uint8_t* scales, uint32_t lds16,
                                                      uint32_t row0, uint32_t units, RowDiv div)
 {
     const uint32_t u = blockIdx.x * kBlock + threadIdx.x;
@@ -105,7 +134,7 @@ __global__ __launch_bounds__(kBlock) void k_mx4_rows(const void* x, int64_t cols
     const uint32_t oct = u - in * div.n;
     const uint32_t row = row0 + in;
     float v[8];
-    load_octet<T>(static_cast<const char*>(x) + row * ldx * kElemBytes<T>, int64_t(oct) * 8, cols, v);
+    load_octet<T>(static_cast<const char*>(x) + row_start(row, ldx16), int64_t(oct) * 8, cols, v);
     uint4 halves;
     if constexpr (SR) {
         const uint32_t k0 = static_cast<uint32_t>(seed), k1 = static_cast<uint32_t>(seed >> 32);
@@ -118,9 +147,9 @@ __global__ __launch_bounds__(kBlock) void k_mx4_rows(const void* x, int64_t cols
     else
         w = mx4_nearest(v, byte);
     w = byte == kMxNaN ? 0u : w;
-    *reinterpret_cast<uint32_t*>(codes + row * ldc + int64_t(oct) * 4) = w;
+    *reinterpret_cast<uint32_t*>(codes + row_start(row, ldc16) + int64_t(oct) * 4) = w;
     if ((oct & 3) == 0)
-        scales[row * lds + oct / 4] = static_cast<uint8_t>(byte);
+        scales[row_start(row, lds16) + oct / 4] = static_cast<uint8_t>(byte);
 }
 
 // Codes of the transposed matrix, and with ROWS of the rows too, from one
@@ -179,13 +208,21 @@ __global__ __launch_bounds__(kBlock) void k_mx4_tiles(const void* x, int64_t row
     {
         const int oc = threadIdx.x & 7, r0 = threadIdx.x >> 3;
         const uint32_t oct = static_cast<uint32_t>(col0 / 8) + oc;
-        float v[4][8];
+        const int64_t row1 = row0 + r0;
+        const char* at = static_cast<const char*>(x) + (row1 * ldx + col0 + oc * 8) * kElemBytes<T>;
+        Octet<T> raw[4];
+        if (row0 + kTileRows <= rows && col0 + kTileCols <= cols) {  // the same in the whole block
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t row = row0 + r0 + 32 * i;
-            load_octet<T>(static_cast<const char*>(x) + row * ldx * kElemBytes<T>, int64_t(oct) * 8,
-                          row < rows ? cols : 0, v[i]);
+            for (int i = 0; i < 4; ++i)
+                raw[i] = read_octet<T>(at + i * 32 * ldx * kElemBytes<T>);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                raw[i] = read_some<T>(at + i * 32 * ldx * kElemBytes<T>, row1 + 32 * i < rows ? cols - col0 - oc * 8 : 0);
         }
+        uint8_t* const code_row = ROWS ? codes + row1 * ldc + int64_t(oct) * 4 : nullptr;
+        uint8_t* const scale_row = ROWS ? scales + row1 * lds + oct / 4 : nullptr;
+        const bool col_ok = col0 + (oc & ~3) * 8 < cols;
         LaneKey lk;
         if constexpr (SR)
             lk = lane_key(oct, 0, k1);
@@ -193,40 +230,42 @@ __global__ __launch_bounds__(kBlock) void k_mx4_tiles(const void* x, int64_t row
         for (int i = 0; i < 4; ++i) {
             const int r = r0 + 32 * i;
             const uint32_t row = static_cast<uint32_t>(row0 + r);
+            float v[8];
+            unpack_octet<T>(raw[i], v);
             uint4 halves = make_uint4(0, 0, 0, 0);
             if constexpr (SR)
                 halves = philox_tail_not(row_key(0, row, k0), lk, k0, k1);
             if constexpr (ROWS) {
-                const uint32_t byte = mx4_byte(quad_max(octet_max(v[i])));
+                const uint32_t byte = mx4_byte(quad_max(octet_max(v)));
                 uint32_t w;
                 if constexpr (SR)
-                    w = mx4_stochastic(v[i], byte, halves, oct, row, seed);
+                    w = mx4_stochastic(v, byte, halves, oct, row, seed);
                 else
-                    w = mx4_nearest(v[i], byte);
-                if (row < rows && (oct & ~3u) * 8 < cols) {
-                    *reinterpret_cast<uint32_t*>(codes + row * ldc + int64_t(oct) * 4) = byte == kMxNaN ? 0u : w;
+                    w = mx4_nearest(v, byte);
+                if (col_ok && row1 + 32 * i < rows) {
+                    *reinterpret_cast<uint32_t*>(code_row + i * 32 * ldc) = byte == kMxNaN ? 0u : w;
                     if ((oct & 3) == 0)
-                        scales[row * lds + oct / 4] = static_cast<uint8_t>(byte);
+                        scale_row[i * 32 * lds] = static_cast<uint8_t>(byte);
                 }
             }
             const uint32_t h[4] = {halves.x, halves.y, halves.z, halves.w};
-            const int at = tile_at(r, oc * 8);
+            const int to = tile_at(r, oc * 8);
             uint32_t d[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                uint32_t e = __float_as_uint(v[i][j]);
+                uint32_t e = __float_as_uint(v[j]);
                 if constexpr (T == kF16) {
-                    const _Float16 f = static_cast<_Float16>(v[i][j]);
+                    const _Float16 f = static_cast<_Float16>(v[j]);
                     e = static_cast<uint32_t>(__builtin_bit_cast(uint16_t, f)) << 16;
                 }
                 if constexpr (T != kF32 && SR)  // bytes 2, 3 of the element, 0, 1 or 2, 3 of the word
                     e = __builtin_amdgcn_perm(e, h[j & 3], j < 4 ? 0x07060100u : 0x07060302u);
                 d[j] = e;
             }
-            *reinterpret_cast<u32x4*>(elems + at) = u32x4{d[0], d[1], d[2], d[3]};
-            *reinterpret_cast<u32x4*>(elems + at + 4) = u32x4{d[4], d[5], d[6], d[7]};
+            *reinterpret_cast<u32x4*>(elems + to) = u32x4{d[0], d[1], d[2], d[3]};
+            *reinterpret_cast<u32x4*>(elems + to + 4) = u32x4{d[4], d[5], d[6], d[7]};
             if constexpr (T == kF32 && SR)
-                *reinterpret_cast<u32x4*>(apart + at) =
+                *reinterpret_cast<u32x4*>(apart + to) =
                     u32x4{(h[0] & 0xFFFFu) | h[1] << 16, (h[2] & 0xFFFFu) | h[3] << 16, h[0] >> 16 | (h[1] & 0xFFFF0000u),
                           h[2] >> 16 | (h[3] & 0xFFFF0000u)};
         }
@@ -303,8 +342,8 @@ __global__ __launch_bounds__(kBlock) void k_mx4_tiles(const void* x, int64_t row
 // once, and give NaN for the scale byte 255.  Values leave nontemporally:
 // 16384 x 8192 bf16 47.4 us, 63.6 with plain stores; 4096^2 5.9 and 7.5.
 template <int T>
-__global__ __launch_bounds__(kBlock) void k_mx4_read(const uint8_t* codes, int64_t ldc, const uint8_t* scales,
-                                                     int64_t lds, int64_t cols, void* out, int64_t ldo,
+__global__ __launch_bounds__(kBlock) void k_mx4_read(const uint8_t* codes, uint32_t ldc16, const uint8_t* scales,
+                                                     uint32_t lds16, int64_t cols, void* out, uint32_t ldo16,
                                                      uint32_t row0, uint32_t units, RowDiv div)
 {
     constexpr int kEach = 16 / kElemBytes<T>;
@@ -313,9 +352,10 @@ __global__ __launch_bounds__(kBlock) void k_mx4_read(const uint8_t* codes, int64
         return;
     const uint32_t in = div_row(u, div);
     const uint32_t at = u - in * div.n;
-    const int64_t row = int64_t(row0) + in, col = int64_t(at) * kEach;
-    const float s = __uint_as_float(static_cast<uint32_t>(scales[row * lds + at / (kMxBlock / kEach)]) << 23);
-    const uint8_t* from = codes + row * ldc + int64_t(at) * (kEach / 2);
+    const uint32_t row = row0 + in;
+    const int64_t col = int64_t(at) * kEach;
+    const float s = __uint_as_float(static_cast<uint32_t>(scales[row_start(row, lds16) + at / (kMxBlock / kEach)]) << 23);
+    const uint8_t* from = codes + row_start(row, ldc16) + int64_t(at) * (kEach / 2);
     u32x4 v;
     if constexpr (T == kF32) {
         const uint32_t w = *reinterpret_cast<const uint16_t*>(from);
@@ -335,7 +375,7 @@ __global__ __launch_bounds__(kBlock) void k_mx4_read(const uint8_t* codes, int64
             v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 3));
         }
     }
-    char* to = static_cast<char*>(out) + (row * ldo + col) * kElemBytes<T>;
+    char* to = static_cast<char*>(out) + row_start(row, ldo16) + col * kElemBytes<T>;
     if (col + kEach <= cols) {
         __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(to));
         return;
@@ -604,6 +644,12 @@ int64_t blocks_for(int64_t units, int64_t per)
     return (units + per - 1) / per;
 }
 
+// A row stride (below 2^36 bytes, as the ABI layer checks) in 16-byte units.
+uint32_t in16(int64_t bytes)
+{
+    return static_cast<uint32_t>(bytes / 16);
+}
+
 // Rows [row0, rows) in launches of at most `cap` blocks and 2^31 units.
 template <typename F>
 hipError_t over_rows(int64_t rows, int64_t per_row, F launch)
@@ -642,7 +688,8 @@ hipError_t quantise(const QuantiseArgs& a, hipStream_t stream)
         const RowDiv div = row_div(static_cast<uint32_t>(per_row));
         return over_rows(a.rows, per_row, [&](uint32_t row0, uint32_t units) {
             k_mx4_rows<T, SR><<<static_cast<unsigned>(blocks_for(units, kBlock)), kBlock, 0, stream>>>(
-                a.x, a.cols, a.ldx, a.seed, a.codes, a.ldc, a.scales, a.lds, row0, units, div);
+                a.x, a.cols, in16(a.ldx * kElemBytes<T>), a.seed, a.codes, in16(a.ldc), a.scales, in16(a.lds), row0, units,
+                div);
         });
     }
     const int32_t down = static_cast<int32_t>(blocks_for(a.rows, kTileRows));
@@ -686,12 +733,9 @@ hipError_t launch_mx4_dequantize(const uint8_t* codes, int64_t ldc, const uint8_
     const RowDiv div = row_div(static_cast<uint32_t>(per_row));
     return over_rows(rows, per_row, [&](uint32_t row0, uint32_t units) {
         const unsigned grid = static_cast<unsigned>(blocks_for(units, kBlock));
-        if (type == kF32)
-            k_mx4_read<kF32><<<grid, kBlock, 0, stream>>>(codes, ldc, scales, lds, cols, out, ldo, row0, units, div);
-        else if (type == kBF16)
-            k_mx4_read<kBF16><<<grid, kBlock, 0, stream>>>(codes, ldc, scales, lds, cols, out, ldo, row0, units, div);
-        else
-            k_mx4_read<kF16><<<grid, kBlock, 0, stream>>>(codes, ldc, scales, lds, cols, out, ldo, row0, units, div);
+        const auto f = type == kF32 ? k_mx4_read<kF32> : type == kBF16 ? k_mx4_read<kBF16> : k_mx4_read<kF16>;
+        f<<<grid, kBlock, 0, stream>>>(codes, in16(ldc), scales, in16(lds), cols, out, in16(ldo * (type == kF32 ? 4 : 2)),
+                                       row0, units, div);
     });
 }
 

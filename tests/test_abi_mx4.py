@@ -50,6 +50,8 @@ def refused(status, want):
     (dict(codes=None, scales=None, codes_t=None, scales_t=None), "inval"),
     (dict(ldc=32), "inval"), (dict(ldc=56), "align"), (dict(codes=A + 4), "align"), (dict(lds=0), "inval"),
     (dict(lds=8), "align"), (dict(scales=A + 1), "align"), (dict(ldct=16), "inval"), (dict(ldct=40), "align"),
+    (dict(ldx=1 << 34), "range"), (dict(type=1, ldx=1 << 35), "range"), (dict(ldc=1 << 36), "range"),
+    (dict(lds=1 << 36), "range"), (dict(ldct=1 << 36), "range"), (dict(ldst=1 << 36), "range"),
     (dict(codes_t=A + 8), "align"), (dict(ldst=1), "inval"), (dict(ldst=24), "align"), (dict(scales_t=A + 2), "align"),
 ])
 def test_quantize_refuses(kw, want):
@@ -61,6 +63,7 @@ def test_quantize_refuses(kw, want):
     (dict(rows=-2), "inval"), (dict(cols=1 << 31), "range"), (dict(ldc=32), "inval"), (dict(ldc=50), "align"),
     (dict(lds=2), "inval"), (dict(lds=20), "align"), (dict(ldo=64), "inval"), (dict(ldo=74), "align"),
     (dict(type=1, ldo=76), "align"), (dict(out=A + 4), "align"), (dict(codes=A + 2), "align"),
+    (dict(ldo=1 << 34), "range"), (dict(ldc=1 << 36), "range"), (dict(lds=1 << 40), "range"),
     (dict(scales=A + 4), "align"),
 ])
 def test_dequantize_refuses(kw, want):
@@ -74,6 +77,7 @@ def test_dequantize_refuses(kw, want):
     (dict(n=1 << 31), "range"), (dict(k=1 << 31), "range"), (dict(type=3), "range"), (dict(accumulate=2), "inval"),
     (dict(lda=32), "inval"), (dict(lda=56), "align"), (dict(ldas=2), "inval"), (dict(ldas=12), "align"),
     (dict(ldb=32), "inval"), (dict(ldb=49), "align"), (dict(ldbs=0), "inval"), (dict(ldbs=17), "align"),
+    (dict(lda=1 << 36), "range"), (dict(ldbs=1 << 36), "range"), (dict(ldo=1 << 34), "range"),
     (dict(ldo=8), "inval"), (dict(ldo=10), "align"), (dict(type=2, ldo=12), "align"), (dict(a=A + 8), "align"),
     (dict(sa=A + 4), "align"), (dict(b=A + 1), "align"), (dict(sb=A + 2), "align"), (dict(out=A + 4), "align"),
 ])
