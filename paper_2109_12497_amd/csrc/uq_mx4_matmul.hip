@@ -23,6 +23,8 @@ struct MatmulPlan {
     int32_t mt, nt;  // 16 rows of a and of b that a block takes (kRows)
 };
 
+constexpr int64_t kMostParted = int64_t(1) << 24;
+
 // Nanoseconds that tiles of 128 x 128 or 256 x 256 take, `stages` stages of 256
 // deep.  Fitted on one MI355X to within 15%: a compute unit holds two small
 // tiles, which take 0.75 us a stage alone and 1.3 together, with 4 us around
@@ -30,20 +32,20 @@ struct MatmulPlan {
 // 1.8 with all compute units at work, which then run slower, with 8 us around
 // it (8192^3 269 us in large tiles, 4096^3 41 in large and 49 in small ones,
 // 2048^3 19 and 11).
-int64_t tiles_ns(int64_t m, int64_t n, int64_t stages, int64_t parts, bool large)
+double tiles_ns(int64_t m, int64_t n, int64_t stages, int64_t parts, bool large)
 {
     if (large) {
         const int64_t blocks = ((m + 255) / 256) * ((n + 255) / 256);
-        const int64_t stage = 1300 + 500 * (blocks < 256 ? blocks : 256) / 256;
-        return (blocks + 255) / 256 * (stages * stage + 8000);
+        const double stage = 1300.0 + 500.0 * static_cast<double>(blocks < 256 ? blocks : 256) / 256.0;
+        return static_cast<double>((blocks + 255) / 256) * (static_cast<double>(stages) * stage + 8000.0);
     }
     const int64_t blocks = ((m + 127) / 128) * ((n + 127) / 128) * parts, rest = blocks % 512;
-    int64_t ns = blocks / 512 * (stages * 1300 + 4000);
+    double ns = static_cast<double>(blocks / 512) * (static_cast<double>(stages) * 1300.0 + 4000.0);
     if (rest > 0)
-        ns += stages * (rest <= 256 ? 750 : 1300) + 4000;
+        ns += static_cast<double>(stages) * (rest <= 256 ? 750.0 : 1300.0) + 4000.0;
     // the parts are written, read again by another launch, and added: 1024 x
     // 1024 x 32768 88 us in one part, 37 in four
-    return parts > 1 ? ns + 6000 + m * n * 8 * parts / 6000 : ns;
+    return parts > 1 ? ns + 6000.0 + static_cast<double>(m * n * parts) / 750.0 : ns;
 }
 
 // Few rows: a block reads mt fragments of a and nt of b.  What takes the time
@@ -55,9 +57,10 @@ MatmulPlan rows_plan(int64_t m, int64_t n)
 {
     MatmulPlan best = {MatmulPlan::kRows, 1, m <= 16 ? 1 : m <= 32 ? 2 : m <= 48 ? 3 : 4, 1};
     const int64_t down = (m + 16 * best.mt - 1) / (16 * best.mt), a = m < 16 * best.mt ? m : 16 * best.mt;
-    int64_t least = 0;
+    double least = 0.0;
     for (int32_t nt = 1; nt <= 4; nt *= 2) {
-        const int64_t blocks = down * ((n + 16 * nt - 1) / (16 * nt)), rows = (blocks + 255) / 256 * (a + 16 * nt);
+        const int64_t blocks = down * ((n + 16 * nt - 1) / (16 * nt));
+        const double rows = static_cast<double>((blocks + 255) / 256) * static_cast<double>(a + 16 * nt);
         if (nt == 1 || rows < least) {
             least = rows;
             best.nt = nt;
@@ -73,10 +76,12 @@ MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
         return rows_plan(m, n);
     const int64_t stages = (k + 255) / 256, batches = (stages + kBatch - 1) / kBatch;
     MatmulPlan best = {MatmulPlan::kTiles256, 1, 0, 0};
-    int64_t least = tiles_ns(m, n, stages, 1, true);
-    for (int32_t parts = 1; parts <= 8 && parts <= batches; parts *= 2) {
+    double least = tiles_ns(m, n, stages, 1, true);
+    // parts of more outputs than this never pay, and bound the workspace (512 MB)
+    const int32_t most = m * n <= kMostParted ? 8 : 1;
+    for (int32_t parts = 1; parts <= most && parts <= batches; parts *= 2) {
         const int64_t deep = parts == 1 ? stages : (batches + parts - 1) / parts * kBatch;
-        const int64_t ns = tiles_ns(m, n, deep, parts, false);
+        const double ns = tiles_ns(m, n, deep, parts, false);
         if (ns < least) {
             least = ns;
             best = {MatmulPlan::kTiles128, parts, 0, 0};
@@ -158,22 +163,17 @@ __device__ __forceinline__ i32x4 buffer_of(const uint8_t* p, int64_t bytes)
                  0x00027000};
 }
 
-// Loads straight into LDS: lane i's 16 (4) bytes go to lds + 16 i (4 i).
-// They have no register results; the waits on them are the caller's
-// (vmcnt), and the compiler, which does not know of them, can only wait for
-// more than it needs.  The s_nop is the wait state between a write of m0 and
-// a load that uses it.
+// A load straight into LDS: lane i's 16 bytes go to lds + 16 i.  It has no
+// register result; the waits on such loads are the caller's (vmcnt), and the
+// compiler, which does not know of them, can only wait for more than it needs.
+// The s_nop is the wait state between a write of m0 and a load that uses it;
+// nothing else in these kernels uses m0 (a reserved register, which the
+// compiler takes in no clobber list).
 __device__ __forceinline__ void load_lds16(i32x4 r, uint32_t off, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(r)
                  : "memory");
 }
-__device__ __forceinline__ void load_lds4(i32x4 r, uint32_t off, uint32_t lds)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(r)
-                 : "memory");
-}
-
 struct MatmulArgs {
     const uint8_t *a, *as, *b, *bs;
     int64_t lda, ldas, ldb, ldbs;
@@ -267,12 +267,18 @@ struct Operand {
     }
 };
 
-// A block of four waves, two by two, forms a tile of 64 FM x 64 FN outputs;
-// a wave holds FM x FN accumulators of 32 x 32.  Lane l holds row l % 32 of
-// an operand's fragment and the blocks 4 (l / 32) + t of a stage for its
+// A block of WM x WN waves forms a tile of 32 WM FM x 32 WN FN outputs; a wave
+// holds FM x FN accumulators of 32 x 32.  Lane l holds row l % 32 of an
+// operand's fragment and the blocks 4 (l / 32) + t of a stage for its
 // instruction t = 0..3: any order of the blocks along k gives the same
 // products as long as both operands keep to it, and in this one a lane's four
 // scale bytes are one dword.
+//   What bounds it, 8192^3 to bf16 on one MI355X: 263 us, 4180 TFLOP/s.  The
+// card lowers its clock by the data: on zeros the same instructions take 187
+// us (5890), and matrix instructions alone reach 6540 on random codes and 9000
+// on zeros.  The rest is the loads into LDS (without them, on random codes, 15%
+// less), and the outputs, which all compute units store at once (4%).  Eight
+// waves of 128 x 64 against four of 128 x 128: 269 and 272 us.
 template <int T, int WM, int WN, int FM, int FN>
 __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx4_tiles(MatmulArgs g)
 {
