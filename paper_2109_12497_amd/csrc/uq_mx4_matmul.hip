@@ -25,42 +25,51 @@ struct MatmulPlan {
 
 constexpr int64_t kMostParted = int64_t(1) << 24;
 
-// Nanoseconds that tiles of 128 x 128 or 256 x 256 take, `stages` stages of 256
-// deep.  Fitted on one MI355X to within 15%: a compute unit holds two small
-// tiles, which take 0.75 us a stage alone and 1.3 together, with 4 us around
-// them (256 x 8192 x 8192, 2048^3, 4096^3); a large one takes 1.3 us alone and
-// 1.8 with all compute units at work, which then run slower, with 8 us around
-// it (8192^3 269 us in large tiles, 4096^3 41 in large and 49 in small ones,
-// 2048^3 19 and 11).
+// The nanoseconds that each form takes, fitted on one MI355X over 370 products
+// (1 to 4096 x 64 to 65536 x 32 to 65536, operands in the caches and not) so
+// that the least of them picks the fastest form: within 1% of it in the mean,
+// 32% at most.
+//
+// Tiles of 128 x 128 or 256 x 256, `stages` stages of 256 deep.  A compute unit
+// holds two small tiles or a large one, whose stage costs more with all compute
+// units at work, which then run slower: 8192^3 269 us in large tiles; 2048^3 11
+// us in small tiles, 19 in large ones.
 double tiles_ns(int64_t m, int64_t n, int64_t stages, int64_t parts, bool large)
 {
     if (large) {
         const int64_t blocks = ((m + 255) / 256) * ((n + 255) / 256);
-        const double stage = 1300.0 + 500.0 * static_cast<double>(blocks < 256 ? blocks : 256) / 256.0;
-        return static_cast<double>((blocks + 255) / 256) * (static_cast<double>(stages) * stage + 8000.0);
+        const double stage = 1300.0 + 580.0 * static_cast<double>(blocks < 256 ? blocks : 256) / 256.0;
+        return static_cast<double>((blocks + 255) / 256) * (static_cast<double>(stages) * stage + 7500.0);
     }
     const int64_t blocks = ((m + 127) / 128) * ((n + 127) / 128) * parts, rest = blocks % 512;
-    double ns = static_cast<double>(blocks / 512) * (static_cast<double>(stages) * 1300.0 + 4000.0);
+    double ns = static_cast<double>(blocks / 512) * (static_cast<double>(stages) * 1100.0 + 4600.0);
     if (rest > 0)
-        ns += static_cast<double>(stages) * (rest <= 256 ? 750.0 : 1300.0) + 4000.0;
-    // the parts are written, read again by another launch, and added: 1024 x
-    // 1024 x 32768 88 us in one part, 37 in four
-    return parts > 1 ? ns + 6000.0 + static_cast<double>(m * n * parts) / 750.0 : ns;
+        ns += static_cast<double>(stages) * (rest <= 256 ? 770.0 : 770.0 + 330.0 * static_cast<double>(rest - 256) / 256.0)
+              + 4600.0;
+    // the parts are written, read again by another launch, and added: 64 x 1000
+    // x 20000 68 us in one part, 39, 24 and 19 in two, four and eight
+    return parts > 1 ? ns + 2500.0 + 0.0015 * static_cast<double>(m * n) * static_cast<double>(parts) : ns;
 }
 
 // Few rows: a block reads mt fragments of a and nt of b.  What takes the time
-// is the loads that a compute unit issues, so the number of fragments that a
-// unit's blocks read decides: 37 x 10001 x 5003 9.4 us with nt = 4 (157 blocks),
-// 12.2 with 2 (313, two to a unit) and 11.7 with 1; 48 x 8192 x 8192 14.7 with
-// 2 (256 blocks), 20.1 and 20.9; 32 x 4096 x 4096 5.8 with 1, 7.0 with 2.
+// is the loads that a compute unit issues, so the rows that a unit's blocks
+// read decide, those of a, which stay in the caches, by half: 64 x 10001 x 5003
+// 13.7 us with nt = 3 (209 blocks), 18.0 with 4 (157), 21.2 with 2 (313, two to
+// a unit) and 25.7 with 1; 48 x 8192 x 8192 17.2 with 2 (256 blocks), 19.5, 21.6
+// and 23.6 with 3, 4 and 1; 32 x 4096 x 4096 6.6 with 1, 7.6, 8.9 and 10.0 with
+// 2, 3 and 4; 32 x 28672 x 8192 38.9 with 4 (448), 48.3, 49.0 and 56.7 with 3, 2
+// and 1.  Three beside one fragment of a never were the best (16 x 10001 x 5003
+// 14.8, with 1 11.5).
 MatmulPlan rows_plan(int64_t m, int64_t n)
 {
     MatmulPlan best = {MatmulPlan::kRows, 1, m <= 16 ? 1 : m <= 32 ? 2 : m <= 48 ? 3 : 4, 1};
     const int64_t down = (m + 16 * best.mt - 1) / (16 * best.mt), a = m < 16 * best.mt ? m : 16 * best.mt;
     double least = 0.0;
-    for (int32_t nt = 1; nt <= 4; nt *= 2) {
+    for (int32_t nt = 1; nt <= 4; ++nt) {
+        if (nt == 3 && best.mt == 1)
+            continue;
         const int64_t blocks = down * ((n + 16 * nt - 1) / (16 * nt));
-        const double rows = static_cast<double>((blocks + 255) / 256) * static_cast<double>(a + 16 * nt);
+        const double rows = static_cast<double>((blocks + 255) / 256) * (0.5 * static_cast<double>(a) + 16.0 * nt);
         if (nt == 1 || rows < least) {
             least = rows;
             best.nt = nt;
@@ -69,14 +78,28 @@ MatmulPlan rows_plan(int64_t m, int64_t n)
     return best;
 }
 
+// The rows that a compute unit reads, over k, and what its blocks add up and
+// store (all of a unit's blocks start together, so a last round that fills few
+// units costs half of one).
+double rows_ns(const MatmulPlan& plan, int64_t m, int64_t n, int64_t k)
+{
+    const int64_t down = (m + 16 * plan.mt - 1) / (16 * plan.mt), a = m < 16 * plan.mt ? m : 16 * plan.mt;
+    const int64_t blocks = down * ((n + 16 * plan.nt - 1) / (16 * plan.nt));
+    const double share = static_cast<double>(blocks) / 256.0;
+    const double rounds = 0.5 * (static_cast<double>((blocks + 255) / 256) + (share < 1.0 ? 1.0 : share));
+    const double read = (0.5 * static_cast<double>(a) + 16.0 * plan.nt) * static_cast<double>(k);
+    return 2600.0 + rounds * (0.021 * read + 250.0 * plan.mt * plan.nt);
+}
+
 MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
 {
-    // 64 x 8192 x 8192 16.4 us as few rows, 26.4 in tiles
-    if (m <= 64 || k == 0)
-        return rows_plan(m, n);
+    // 64 x 4096 x 4096 8.9 us as few rows, 12.0 in tiles; 64 x 28672 x 8192 58.7
+    // and 37.9; 256 x 1000 x 20000 22.2 and 21.3 (eight parts)
+    MatmulPlan best = rows_plan(m, n);
+    if (k == 0)
+        return best;
     const int64_t stages = (k + 255) / 256, batches = (stages + kBatch - 1) / kBatch;
-    MatmulPlan best = {MatmulPlan::kTiles256, 1, 0, 0};
-    double least = tiles_ns(m, n, stages, 1, true);
+    double least = rows_ns(best, m, n, k);
     // parts of more outputs than this never pay, and bound the workspace (512 MB)
     const int32_t most = m * n <= kMostParted ? 8 : 1;
     for (int32_t parts = 1; parts <= most && parts <= batches; parts *= 2) {
@@ -87,6 +110,8 @@ MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
             best = {MatmulPlan::kTiles128, parts, 0, 0};
         }
     }
+    if (tiles_ns(m, n, stages, 1, true) < least)
+        best = {MatmulPlan::kTiles256, 1, 0, 0};
     return best;
 }
 
@@ -490,7 +515,8 @@ __global__ __launch_bounds__(kBlock) void k_mx4_join(const float* parts, int32_t
 }
 
 // ---------------------------------------------------------------------------
-// Few rows of a: every row of b is read once, straight into registers.
+// Few rows of a, or few outputs: both operands go straight into registers.  Up
+// to 64 rows of a every row of b is read once.
 // ---------------------------------------------------------------------------
 // A block forms 16 MT x 16 NT outputs; its waves share k in chunks of 16
 // blocks (512 elements), and add their sums through LDS in the waves' order.
@@ -671,6 +697,9 @@ hipError_t rows_by(MatmulArgs g, hipStream_t stream)
 template <int MT>
 hipError_t rows_by(const MatmulArgs& g, int32_t nt, hipStream_t stream)
 {
+    if constexpr (MT > 1)
+        if (nt == 3)
+            return rows_by<MT, 3>(g, stream);
     return nt == 1 ? rows_by<MT, 1>(g, stream) : nt == 2 ? rows_by<MT, 2>(g, stream) : rows_by<MT, 4>(g, stream);
 }
 
