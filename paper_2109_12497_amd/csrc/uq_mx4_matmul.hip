@@ -116,52 +116,71 @@ MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
 }
 
 // The element at `at` of the output, of type `type` (the same for the whole launch).
-__device__ __forceinline__ void store_out(int32_t type, void* out, int64_t at, float v, bool accumulate)
+__device__ __forceinline__ float load_out(int32_t type, const void* out, int64_t at)
 {
-    if (type == kF32) {
-        float* o = static_cast<float*>(out) + at;
-        *o = accumulate ? *o + v : v;
-    } else if (type == kBF16) {
-        __bf16* o = static_cast<__bf16*>(out) + at;
-        *o = static_cast<__bf16>(accumulate ? static_cast<float>(*o) + v : v);
-    } else {
-        _Float16* o = static_cast<_Float16*>(out) + at;
-        *o = static_cast<_Float16>(accumulate ? static_cast<float>(*o) + v : v);
-    }
+    return type == kF32 ? static_cast<const float*>(out)[at]
+         : type == kBF16 ? static_cast<float>(static_cast<const __bf16*>(out)[at])
+                         : static_cast<float>(static_cast<const _Float16*>(out)[at]);
 }
 
-// Columns col .. col + 3 (a multiple of 4) of the row that starts at `row`.
+__device__ __forceinline__ void store_out(int32_t type, void* out, int64_t at, float v)
+{
+    if (type == kF32)
+        static_cast<float*>(out)[at] = v;
+    else if (type == kBF16)
+        static_cast<__bf16*>(out)[at] = static_cast<__bf16>(v);
+    else
+        static_cast<_Float16*>(out)[at] = static_cast<_Float16>(v);
+}
+
+// Four columns of the output as they lie in memory, and their values.
 template <int T>
-__device__ __forceinline__ void store_four(void* out, int64_t row, int64_t col, int64_t n, f32x4 v, bool accumulate)
+using Four = std::conditional_t<T == kF32, f32x4, u32x2>;
+
+template <int T>
+__device__ __forceinline__ f32x4 values(Four<T> x)
+{
+    if constexpr (T == kF32)
+        return x;
+    const uint32_t x0 = x[0], x1 = x[1];
+    if constexpr (T == kBF16)
+        return f32x4{__uint_as_float(x0 << 16), __uint_as_float(x0 & 0xFFFF0000u), __uint_as_float(x1 << 16),
+                     __uint_as_float(x1 & 0xFFFF0000u)};
+    const f16x2 a = __builtin_bit_cast(f16x2, x0), b = __builtin_bit_cast(f16x2, x1);
+    return f32x4{static_cast<float>(a[0]), static_cast<float>(a[1]), static_cast<float>(b[0]), static_cast<float>(b[1])};
+}
+
+// Columns col .. col + 3 (a multiple of 4) of the row that starts at `row`, of
+// n; `old` is what load_four read there before.
+template <int T>
+__device__ __forceinline__ Four<T> load_four(const void* out, int64_t row, int64_t col, int64_t n)
+{
+    using Element = std::conditional_t<T == kF32, float, uint16_t>;
+    return col + 4 > n ? Four<T>{} : *reinterpret_cast<const Four<T>*>(static_cast<const Element*>(out) + row + col);
+}
+
+template <int T>
+__device__ __forceinline__ void store_four(void* out, int64_t row, int64_t col, int64_t n, f32x4 v, bool accumulate,
+                                           Four<T> old)
 {
     if (col + 4 > n) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (col + j < n)
-                store_out(T, out, row + col + j, v[j], accumulate);
+                store_out(T, out, row + col + j, accumulate ? load_out(T, out, row + col + j) + v[j] : v[j]);
         return;
     }
+    if (accumulate)
+        v += values<T>(old);
     if constexpr (T == kF32) {
-        f32x4* o = reinterpret_cast<f32x4*>(static_cast<float*>(out) + row + col);
-        *o = accumulate ? *o + v : v;
+        *reinterpret_cast<f32x4*>(static_cast<float*>(out) + row + col) = v;
     } else {
         u32x2* o = reinterpret_cast<u32x2*>(static_cast<uint16_t*>(out) + row + col);
         if constexpr (T == kBF16) {
-            if (accumulate) {
-                const u32x2 old = *o;
-                v += f32x4{__uint_as_float(old[0] << 16), __uint_as_float(old[0] & 0xFFFF0000u),
-                           __uint_as_float(old[1] << 16), __uint_as_float(old[1] & 0xFFFF0000u)};
-            }
             const bf16x2 a = {static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1])};
             const bf16x2 b = {static_cast<__bf16>(v[2]), static_cast<__bf16>(v[3])};
             *o = u32x2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
         } else {
-            if (accumulate) {
-                const uint32_t o0 = (*o)[0], o1 = (*o)[1];
-                const f16x2 a = __builtin_bit_cast(f16x2, o0), b = __builtin_bit_cast(f16x2, o1);
-                v += f32x4{static_cast<float>(a[0]), static_cast<float>(a[1]), static_cast<float>(b[0]),
-                           static_cast<float>(b[1])};
-            }
             const f16x2 a = {static_cast<_Float16>(v[0]), static_cast<_Float16>(v[1])};
             const f16x2 b = {static_cast<_Float16>(v[2]), static_cast<_Float16>(v[3])};
             *o = u32x2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
@@ -471,27 +490,45 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx4_tiles(MatmulArgs g)
     }
     // Out through LDS, 32 rows of the wave's columns at a time, so that a lane
     // stores four columns.  Rows are kPitch floats apart: the two halves of a
-    // wave, four rows apart, then write different banks.
-    constexpr int kCols = 32 * FN, kPitch = kCols + 8, kLanes = kCols / 4;
-    static_assert(W * 32 * kPitch * 4 <= sizeof(smem) && kPitch % 16 == 8, "the waves' parts fit the stages");
+    // wave, four rows apart, then write different banks.  What the sums are
+    // added to is read 64 rows ahead (4096 x 4096 x 8192 to fp32 88 us, 95 where a
+    // row's are read before its store).
+    constexpr int kCols = 32 * FN, kPitch = kCols + 8, kLanes = kCols / 4, kTurns = 32 * kLanes / 64;
+    static_assert(FM >= 2 && W * 32 * kPitch * 4 <= sizeof(smem) && kPitch % 16 == 8, "the waves' parts fit the stages");
     sync();
     float* mine = reinterpret_cast<float*>(smem) + wave * 32 * kPitch;
-    const int64_t col = col0 + wn * kCols + (lane % kLanes) * 4;
+    const int64_t col = col0 + wn * kCols + (lane % kLanes) * 4, first = row0 + wm * 32 * FM + lane / kLanes;
+    const bool add = g.accumulate != 0;
+    Four<T> old[3][kTurns];
+    const auto load_old = [&](int i) {
+#pragma unroll
+        for (int r = 0; r < kTurns; ++r) {
+            const int64_t row = first + 32 * i + r * (64 / kLanes);
+            if (row < g.m)
+                old[i % 3][r] = load_four<T>(out, row * g.ldo, col, g.n);
+        }
+    };
+    if (add) {
+        load_old(0);
+        load_old(1);
+    }
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
+        if (add && i + 2 < FM)
+            load_old(i + 2);
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 mine[((r & 3) + 8 * (r >> 2) + 4 * half) * kPitch + 32 * j + (lane & 31)] = acc[i][j][r];
         __builtin_amdgcn_wave_barrier();
-        const int64_t first = row0 + wm * 32 * FM + 32 * i;
 #pragma unroll
-        for (int r = 0; r < 32; r += 64 / kLanes) {
-            const int row = r + lane / kLanes;
-            const f32x4 v = *reinterpret_cast<const f32x4*>(mine + row * kPitch + (lane % kLanes) * 4);
-            if (first + row < g.m)
-                store_four<T>(out, (first + row) * g.ldo, col, g.n, v, g.accumulate != 0);
+        for (int r = 0; r < kTurns; ++r) {
+            const int at = r * (64 / kLanes);
+            const f32x4 v = *reinterpret_cast<const f32x4*>(mine + (at + lane / kLanes) * kPitch + (lane % kLanes) * 4);
+            const int64_t row = first + 32 * i + at;
+            if (row < g.m)
+                store_four<T>(out, row * g.ldo, col, g.n, v, add, old[i % 3][r]);
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -508,10 +545,11 @@ __global__ __launch_bounds__(kBlock) void k_mx4_join(const float* parts, int32_t
         return;
     const uint32_t in = div_row(u, div);
     const int64_t row = row0 + in, col = int64_t(u - in * div.n) * 4;
+    const Four<T> old = accumulate != 0 ? load_four<T>(out, row * ldo, col, n) : Four<T>{};
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int32_t c = 0; c < count; ++c)
         v += *reinterpret_cast<const f32x4*>(parts + (c * m + row) * ldp + col);
-    store_four<T>(out, row * ldo, col, n, v, accumulate != 0);
+    store_four<T>(out, row * ldo, col, n, v, accumulate != 0, old);
 }
 
 // ---------------------------------------------------------------------------
@@ -625,16 +663,33 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_mx4_rows_by(MatmulArgs g)
     __syncthreads();
     for (int f = wave; f < MT * NT; f += waves) {
         const int i = f / NT, j = f % NT;
+        const int64_t row = row0 + 16 * i + 4 * q, col = col0 + 16 * j + (lane & 15);
         f32x4 v = part[0][i][j][lane];
         for (int w = 1; w < waves; ++w)
             v += part[w][i][j][lane];
-        const int64_t col = col0 + 16 * j + (lane & 15);
+        // all four are read before one is stored
+        const auto finish = [&](auto type) {
+            constexpr int T = decltype(type)::value;
+            float old[4];
+            if (g.accumulate != 0) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int64_t row = row0 + 16 * i + 4 * q + r;
-            if (row < g.m && col < g.n)
-                store_out(g.type, g.out, row * g.ldo + col, v[r], g.accumulate != 0);
-        }
+                for (int r = 0; r < 4; ++r)
+                    old[r] = row + r < g.m && col < g.n ? load_out(T, g.out, (row + r) * g.ldo + col) : 0.0f;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    v[r] += old[r];
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (row + r < g.m && col < g.n)
+                    store_out(T, g.out, (row + r) * g.ldo + col, v[r]);
+        };
+        if (g.type == kF32)
+            finish(std::integral_constant<int, kF32>{});
+        else if (g.type == kBF16)
+            finish(std::integral_constant<int, kBF16>{});
+        else
+            finish(std::integral_constant<int, kF16>{});
     }
 }
 
