@@ -320,10 +320,12 @@ __global__ __launch_bounds__(kBlock) void k_mx4_tiles(const void* x, int64_t row
 #pragma unroll 1
                 for (int j = 0; j < 8; ++j) {  // each element has a block of low halves of its own
                     const int r = 32 * q + 8 * i + j, at = tile_at(r, c);
-                    const uint32_t e = elems[at];
+                    const uint32_t e = elems[at], half = T == kF32 ? apart[at] : e;
+                    if (byte < kMxTop && mx4_undecided(mx4_carry<0>(value(e), place, half)) >= kUndecided)
+                        continue;  // (8192 x 8192 62 us where all eight were formed, 59)
                     const uint4 lo = philox4x32_10(static_cast<uint32_t>(col >> 3), 0, static_cast<uint32_t>(row0) + r,
                                                    1, k0, k1);
-                    const uint32_t hi = ~(T == kF32 ? apart[at] : e) << 16;
+                    const uint32_t hi = ~half << 16;
                     const uint32_t code = mx4_exact(value(e), mx4_half_units(byte), hi | philox_half(lo, col & 7));
                     w[i] = (w[i] & ~(7u << (4 * j))) | code << (4 * j);
                 }
