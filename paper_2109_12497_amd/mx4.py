@@ -7,6 +7,8 @@ to the current stream of the device the buffers are on, or to the one given.
 """
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 from . import (UQ_BF16, UQ_F16, UQ_F32, _stream, uq_mx4_aggregate, uq_mx4_matmul, uq_mx4_matmul_workspace_bytes, uq_mx4_quantize,
@@ -21,6 +23,20 @@ def _device(device) -> torch.device:
     if device.type == "cuda" and device.index is None:
         device = torch.device("cuda", torch.cuda.current_device())
     return device
+
+
+def _settle(device) -> None:
+    """Waits for the fills of new buffers, which the first call may use on
+    another stream."""
+    if device.type == "cuda" and not torch.cuda.is_current_stream_capturing():
+        torch.cuda.current_stream(device).synchronize()
+
+
+def _on(stream: int | None):
+    """torch's current stream set to a raw handle (None or the current one: as it is)."""
+    if stream is None or stream == _stream(None):
+        return contextlib.nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream())
 
 
 def _check_matrix(t, rows: int, cols: int, device) -> None:
@@ -86,20 +102,24 @@ class Mx4Linear:
             self.dy_t = Codes(outputs, tokens, dev)
             self.dx = torch.zeros((tokens, round_up(inputs, 8)), dtype=dtype, device=dev)
             self.dw = torch.zeros((outputs, round_up(inputs, 4)), dtype=torch.float32, device=dev)
-        self.ws, self._kept = torch.zeros(256, dtype=torch.uint8, device=dev), []
+        self.ws, self._kept = torch.empty(256, dtype=torch.uint8, device=dev), []
         self._reserve(tokens)
         self.rows = 0  # of the last forward
+        _settle(dev)
 
-    def _reserve(self, rows: int) -> None:
+    def _reserve(self, rows: int, stream: int | None = None) -> None:
         """Workspace for the products of `rows` tokens (fewer tokens can need
-        more: k is split where tiles are few), kept for later calls."""
+        more: k is split where tiles are few), kept for later calls.  It is
+        allocated on the stream that will use it, and not cleared: what ran on
+        that memory before, or a fill on another stream, would race."""
         need = [uq_mx4_matmul_workspace_bytes(rows, self.outputs, self.inputs)]
         if self.train:
             need += [uq_mx4_matmul_workspace_bytes(rows, self.inputs, self.outputs),
                      uq_mx4_matmul_workspace_bytes(self.outputs, self.inputs, rows)]
         if max(need) > self.ws.numel():
             self._kept.append(self.ws)  # a captured graph may still use it
-            self.ws = torch.zeros(max(need), dtype=torch.uint8, device=self.device)
+            with _on(stream):
+                self.ws = torch.empty(max(need), dtype=torch.uint8, device=self.device)
 
     def _matmul(self, a: Codes, b: Codes, m: int, n: int, k: int, out, accumulate: bool, stream) -> None:
         uq_mx4_matmul(*a.args(), *b.args(), m, n, k, TYPES[out.dtype], out, out.stride(0), int(accumulate), self.ws,
@@ -115,7 +135,7 @@ class Mx4Linear:
         assert rows <= self.tokens
         _check_matrix(x, rows, self.inputs, self.device)
         stream = _stream(stream)  # resolved once for the calls
-        self._reserve(rows)
+        self._reserve(rows, stream)
         self.rows = rows
         quantize(x, self.x, self.x_t if self.train else None, stream=stream)
         self._matmul(self.x, self.w, rows, self.outputs, self.inputs, self.y, False, stream)
@@ -152,6 +172,7 @@ class Mx4Step:
         self.scales = torch.zeros(round_up(max(-(-d // 32), 1), 16), dtype=torch.uint8, device=self.device)
         self.sum = torch.zeros(round_up(max(d, 1), 64), dtype=torch.int32, device=self.device)
         self.out = torch.zeros(round_up(max(d, 1), 64), dtype=torch.float32, device=self.device)
+        _settle(self.device)
 
     def run(self, g, seed: int, stream=None):
         """g: [M, ldg] float32 on the device.  Returns the output view [d]."""

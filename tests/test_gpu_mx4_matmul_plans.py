@@ -139,3 +139,35 @@ def test_one_matrix_as_both_operands():
     torch.cuda.synchronize()
     v = torch.from_numpy(a[2])
     assert torch.equal(out[:, :1270].cpu().double(), v @ v.t())
+
+
+def test_layer_that_grows_its_workspace_on_a_given_stream():
+    """Fewer rows whose k is split need more workspace than the layer was made
+    for; it is taken while the current stream is busy and the call goes to
+    another one, given as a handle, then as a Stream, then as the default."""
+    from oracle import mx4
+    from paper_2109_12497_amd.mx4 import Mx4Linear
+
+    tokens, rows, inputs, outputs = 4096, 512, 16384, 1000
+    assert uq.uq_mx4_matmul_workspace_bytes(rows, outputs, inputs) > uq.uq_mx4_matmul_workspace_bytes(
+        tokens, outputs, inputs)
+    gen = torch.Generator().manual_seed(3)
+    xh, wh = (torch.randint(-6, 7, (n, inputs), generator=gen).float() for n in (rows, outputs))
+    x, w = xh.to(DEV), wh.to(DEV)
+    busy = torch.randn(4096, 4096, device=DEV)
+
+    def seen(v):
+        codes, scales = mx4.quantize(v.numpy())
+        return torch.from_numpy(mx4.decode(codes, scales, inputs))
+
+    want = seen(xh) @ seen(wh).t()  # multiples of 1 below 2^24
+    side = torch.cuda.Stream()
+    for stream in (side.cuda_stream, side, torch.cuda.default_stream(), None):
+        layer = Mx4Linear(tokens, inputs, outputs, device=DEV, train=False)
+        torch.cuda.synchronize()
+        for _ in range(8):
+            busy = torch.sin(busy)
+        layer.load(w, stream=stream)
+        y = layer.forward(x, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(y.cpu().double(), want)
