@@ -18,37 +18,51 @@ constexpr int kBatch = 4;  // stages of 256 along k whose scale bytes a tile loa
 // Which form a product takes; it goes by the sizes alone, and so does the
 // order of its sums.
 struct MatmulPlan {
-    enum Form { kRows, kTiles128, kTiles256 } form;
-    int32_t parts;   // of k, added afterwards (kTiles128)
+    enum Form { kRows, kTiles64, kTiles128, kTiles256 } form;
+    int32_t parts;   // of k, added afterwards (kTiles64, kTiles128)
     int32_t mt, nt;  // 16 rows of a and of b that a block takes (kRows)
 };
 
 constexpr int64_t kMostParted = int64_t(1) << 24;
 
-// The nanoseconds that each form takes, fitted on one MI355X over 370 products
-// (1 to 4096 x 64 to 65536 x 32 to 65536, operands in the caches and not) so
-// that the least of them picks the fastest form: within 1% of it in the mean,
-// 32% at most.
-//
-// Tiles of 128 x 128 or 256 x 256, `stages` stages of 256 deep.  A compute unit
-// holds two small tiles or a large one, whose stage costs more with all compute
-// units at work, which then run slower: 8192^3 269 us in large tiles; 2048^3 11
-// us in small tiles, 19 in large ones.
-double tiles_ns(int64_t m, int64_t n, int64_t stages, int64_t parts, bool large)
+constexpr int64_t kUnits = 256;  // compute units
+
+int64_t tile_blocks(int64_t m, int64_t n, MatmulPlan::Form form)
 {
-    if (large) {
-        const int64_t blocks = ((m + 255) / 256) * ((n + 255) / 256);
-        const double stage = 1300.0 + 580.0 * static_cast<double>(blocks < 256 ? blocks : 256) / 256.0;
-        return static_cast<double>((blocks + 255) / 256) * (static_cast<double>(stages) * stage + 7500.0);
+    const int64_t high = form == MatmulPlan::kTiles64 ? 64 : form == MatmulPlan::kTiles128 ? 128 : 256;
+    const int64_t wide = form == MatmulPlan::kTiles256 ? 256 : 128;
+    return ((m + high - 1) / high) * ((n + wide - 1) / wide);
+}
+
+// The nanoseconds that each form takes, fitted on one MI355X over 460 products
+// (1 to 4096 x 64 to 65536 x 32 to 65536, operands in the caches and not) so
+// that the least of them picks the fastest form: within 0.6% of it in the mean,
+// 18% at most.
+//
+// Tiles, `stages` stages of 256 deep: a stage costs more with more compute units
+// at work, for they share the caches' bandwidth and then run slower.  8192^3
+// 267 us in tiles of 256 x 256; 2048^3 10.7 us in 128 x 128, 19 in 256 x 256; 192 x
+// 4096 x 4096 10.9 in 64 x 128, 14.0 in 128 x 128.
+double tiles_ns(int64_t m, int64_t n, int64_t stages, int64_t parts, MatmulPlan::Form form)
+{
+    const int64_t blocks = tile_blocks(m, n, form) * parts;
+    const double deep = static_cast<double>(stages), share = static_cast<double>(blocks) / kUnits;
+    // the parts are written, read again by another launch, and added: 200 x 1000
+    // x 20000 36 us in one part, 24, 17.5 and 16 in two, four and eight
+    const double join = parts > 1 ? 2700.0 + 0.001 * static_cast<double>(m * n) * static_cast<double>(parts) : 0.0;
+    switch (form) {
+    case MatmulPlan::kTiles64: return join + deep * (350.0 + 150.0 * share) + 4900.0;
+    case MatmulPlan::kTiles128: {
+        if (blocks <= kUnits)
+            return join + deep * (520.0 + 280.0 * share) + 4900.0;
+        const int64_t rounds = blocks / (2 * kUnits), rest = blocks % (2 * kUnits);
+        const double last = rest > 0 ? deep * 1500.0 * (0.5 + 0.5 * static_cast<double>(rest) / (2 * kUnits)) + 5700.0 : 0.0;
+        return join + static_cast<double>(rounds) * (deep * 1500.0 + 5700.0) + last;
     }
-    const int64_t blocks = ((m + 127) / 128) * ((n + 127) / 128) * parts, rest = blocks % 512;
-    double ns = static_cast<double>(blocks / 512) * (static_cast<double>(stages) * 1100.0 + 4600.0);
-    if (rest > 0)
-        ns += static_cast<double>(stages) * (rest <= 256 ? 770.0 : 770.0 + 330.0 * static_cast<double>(rest - 256) / 256.0)
-              + 4600.0;
-    // the parts are written, read again by another launch, and added: 64 x 1000
-    // x 20000 68 us in one part, 39, 24 and 19 in two, four and eight
-    return parts > 1 ? ns + 2500.0 + 0.0015 * static_cast<double>(m * n) * static_cast<double>(parts) : ns;
+    default:
+        return static_cast<double>((blocks + kUnits - 1) / kUnits) *
+               (deep * (1200.0 + 600.0 * (share < 1.0 ? share : 1.0)) + 11000.0);
+    }
 }
 
 // Few rows: a block reads mt fragments of a and nt of b.  What takes the time
@@ -88,13 +102,13 @@ double rows_ns(const MatmulPlan& plan, int64_t m, int64_t n, int64_t k)
     const double share = static_cast<double>(blocks) / 256.0;
     const double rounds = 0.5 * (static_cast<double>((blocks + 255) / 256) + (share < 1.0 ? 1.0 : share));
     const double read = (0.5 * static_cast<double>(a) + 16.0 * plan.nt) * static_cast<double>(k);
-    return 2600.0 + rounds * (0.021 * read + 250.0 * plan.mt * plan.nt);
+    return 1800.0 + rounds * (0.02 * read + 220.0 * plan.mt * plan.nt);
 }
 
 MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
 {
-    // 64 x 4096 x 4096 8.9 us as few rows, 12.0 in tiles; 64 x 28672 x 8192 58.7
-    // and 37.9; 256 x 1000 x 20000 22.2 and 21.3 (eight parts)
+    // 64 x 4096 x 4096 8.9 us as few rows, 10.4 in tiles; 64 x 28672 x 8192 58 and
+    // 31; 256 x 1000 x 20000 22 and 16 (eight parts)
     MatmulPlan best = rows_plan(m, n);
     if (k == 0)
         return best;
@@ -104,13 +118,19 @@ MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
     const int32_t most = m * n <= kMostParted ? 8 : 1;
     for (int32_t parts = 1; parts <= most && parts <= batches; parts *= 2) {
         const int64_t deep = parts == 1 ? stages : (batches + parts - 1) / parts * kBatch;
-        const double ns = tiles_ns(m, n, deep, parts, false);
-        if (ns < least) {
-            least = ns;
-            best = {MatmulPlan::kTiles128, parts, 0, 0};
+        for (const auto form : {MatmulPlan::kTiles64, MatmulPlan::kTiles128}) {
+            // tiles of 64 x 128 are for a single round: 1024 x 4096 x 4096 20.1
+            // us in two, 16.5 in one of 128 x 128
+            if (form == MatmulPlan::kTiles64 && tile_blocks(m, n, form) * parts > kUnits)
+                continue;
+            const double ns = tiles_ns(m, n, deep, parts, form);
+            if (ns < least) {
+                least = ns;
+                best = {form, parts, 0, 0};
+            }
         }
     }
-    if (tiles_ns(m, n, stages, 1, true) < least)
+    if (tiles_ns(m, n, stages, 1, MatmulPlan::kTiles256) < least)
         best = {MatmulPlan::kTiles256, 1, 0, 0};
     return best;
 }
@@ -259,9 +279,12 @@ constexpr int kBatchBytes = kBatch * kStageBlocks;
 template <int ROWS, int W>
 struct Operand {
     static constexpr int kCodes = ROWS * kStageBytes, kScales = ROWS * kBatchBytes;
-    static constexpr int kStep = 8 * W, kLoads = ROWS / kStep;                  // of a wave, a stage's codes
-    static constexpr int kScaleStep = 32 * W, kScaleLoads = ROWS / kScaleStep;  // and a batch's scales
-    static_assert(ROWS % kScaleStep == 0, "a wave loads the scales of 32 rows at a time");
+    static constexpr int kStep = 8 * W, kLoads = ROWS / kStep;  // of a wave, a stage's codes
+    // and a batch's scales, 32 rows at a time (waves past the rows load what
+    // others do)
+    static constexpr int kScaleWaves = ROWS / 32 < W ? ROWS / 32 : W;
+    static constexpr int kScaleStep = 32 * kScaleWaves, kScaleLoads = ROWS / kScaleStep;
+    static_assert(ROWS % kStep == 0 && ROWS % kScaleStep == 0, "every load is whole");
 
     const uint8_t *p, *s;
     uint32_t ld, ld_s, to, to_s;  // to, to_s: where this wave's parts go in LDS
@@ -279,11 +302,11 @@ struct Operand {
         ld_s = static_cast<uint32_t>(lds);
         bytes = have * ldc - kb0 * kMxBlockBytes;
         bytes_s = have * lds - kb0;
-        const int row = wave * 8 + (lane >> 3), srow = wave * 32 + (lane >> 1);
+        const int row = wave * 8 + (lane >> 3), srow = wave % kScaleWaves * 32 + (lane >> 1);
         off = row * ld + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
         off_s = srow * ld_s + (((lane & 1) ^ ((srow >> 3) & 1)) << 4);
         to = lds_codes + wave * 8 * kStageBytes;
-        to_s = lds_scales + wave * 32 * kBatchBytes;
+        to_s = lds_scales + wave % kScaleWaves * 32 * kBatchBytes;
     }
     // Blocks past the last (nkb) read as 0.
     __device__ __forceinline__ uint32_t offset(int64_t kb, int64_t nkb, int wave, int lane) const
@@ -323,17 +346,17 @@ struct Operand {
 // on zeros.  The rest is the loads into LDS (without them, on random codes, 15%
 // less), and the outputs, which all compute units store at once (4%).  Eight
 // waves of 128 x 64 against four of 128 x 128: 269 and 272 us.
-template <int T, int WM, int WN, int FM, int FN>
+template <int T, int WM, int WN, int FM, int FN, int NS>
 __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx4_tiles(MatmulArgs g)
 {
     constexpr int W = WM * WN, BM = 32 * WM * FM, BN = 32 * WN * FN;
     using A = Operand<BM, W>;
     using B = Operand<BN, W>;
     constexpr int kStage = A::kCodes + B::kCodes, kScaleBatch = A::kScales + B::kScales;
-    __shared__ __attribute__((aligned(128))) uint8_t smem[2 * (kStage + kScaleBatch)];
+    __shared__ __attribute__((aligned(128))) uint8_t smem[NS * kStage + 2 * kScaleBatch];
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
         (__attribute__((address_space(3))) uint8_t*)smem));
-    constexpr int kScalesAt = 2 * kStage;
+    constexpr int kScalesAt = NS * kStage;
 
     const int tiles = g.tiles_m * g.tiles_n, block = g.first + blockIdx.x, part = __builtin_amdgcn_readfirstlane(block / tiles);
     int tm, tn;
@@ -360,7 +383,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx4_tiles(MatmulArgs g)
     const auto codes_of = [&](int64_t stage) {
         const int64_t kb = stage * kStageBlocks;
         return Codes{a.codes_from(kb), b.codes_from(kb), a.offset(kb, nkb, wave, lane), b.offset(kb, nkb, wave, lane),
-                     static_cast<uint32_t>(stage & 1) * kStage};
+                     static_cast<uint32_t>(stage & (NS - 1)) * kStage};
     };
     const auto load_codes = [&](const Codes& c, int j) {
         if (j < A::kLoads)
@@ -381,10 +404,10 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx4_tiles(MatmulArgs g)
                    of_b ? b.off_s + j * B::kScaleStep * b.ld_s : a.off_s + j * A::kScaleStep * a.ld_s,
                    (of_b ? b.to_s : a.to_s) + buf + j * A::kScaleStep * kBatchBytes);
     };
-    // every load into LDS and every read of it by this wave is done, then the
-    // other waves' are
-    const auto sync = [] {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    // every load into LDS but the last `later` and every read of it by this
+    // wave is done, then the other waves' are
+    const auto sync = [](auto later) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(later)::value) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
@@ -393,10 +416,10 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx4_tiles(MatmulArgs g)
     i32x4 fa[2][FM], fb[2][FN];
     uint32_t sa[2][FM], sb[2][FN];
     const auto read_a = [&](int64_t stage, int t, int i) {
-        return A::piece(smem + (stage & 1) * kStage, ar + 32 * i, 4 * half + t);
+        return A::piece(smem + (stage & (NS - 1)) * kStage, ar + 32 * i, 4 * half + t);
     };
     const auto read_b = [&](int64_t stage, int t, int j) {
-        return B::piece(smem + (stage & 1) * kStage + A::kCodes, br + 32 * j, 4 * half + t);
+        return B::piece(smem + (stage & (NS - 1)) * kStage + A::kCodes, br + 32 * j, 4 * half + t);
     };
     const auto read_scales = [&](int64_t stage, uint32_t(&xa)[FM], uint32_t(&xb)[FN]) {
         const uint8_t* l = smem + kScalesAt + ((stage / kBatch) & 1) * kScaleBatch;
@@ -422,25 +445,30 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx4_tiles(MatmulArgs g)
 
     // A stage is four instructions' depth; each is cut into FM groups of FN
     // instructions, with a group's share of the next depth's reads and of the
-    // loads of the stage after next between them: a wave waits for its loads
-    // to be taken, so they are spread.  They go into the half of LDS that the
-    // current stage leaves at its fourth depth, start there and end two depths
-    // into the next stage.  Stages past the last read as zeros, past every
-    // operand's end, and enter no product.
+    // loads of a later stage between them: a wave waits for its loads to be
+    // taken, so they are spread.  LDS holds NS stages; the loads go into the
+    // part that the current stage leaves at its fourth depth, start there and
+    // end two depths into the next stage.  Stages past the last read as zeros,
+    // past every operand's end, and enter no product.
     constexpr int kLoads = A::kLoads + B::kLoads, kSlots = 3 * FM, kPer = (kLoads + kSlots - 1) / kSlots;
     Codes next = codes_of(0);
 #pragma unroll
     for (int i = 0; i < kScaleLoads; ++i)
         load_scales(0, i);
-#pragma unroll
-    for (int l = 0; l < kLoads; ++l)
-        load_codes(next, l);
-    sync();
-    next = codes_of(1);
     load_scales(1, 0);
 #pragma unroll
-    for (int l = 0; l < kLoads && l < FM * kPer; ++l)  // what a stage before would have loaded at its fourth depth
+    for (int st = 0; st < NS - 1; ++st) {
+        next = codes_of(st);
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l)
+            load_codes(next, l);
+    }
+    next = codes_of(NS - 1);
+    constexpr int kFirst = FM * kPer < kLoads ? FM * kPer : kLoads;  // at a stage's fourth depth
+#pragma unroll
+    for (int l = 0; l < kFirst; ++l)
         load_codes(next, l);
+    sync(std::integral_constant<int, (NS - 2) * kLoads + kFirst>{});
     read_scales(0, sa[0], sb[0]);
     keep_scales(0, sa[0], sb[0]);
 #pragma unroll
@@ -475,9 +503,13 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx4_tiles(MatmulArgs g)
         depth(std::integral_constant<int, 0>{}, s);
         depth(std::integral_constant<int, 1>{}, s);
         depth(std::integral_constant<int, 2>{}, s);
-        sync();  // stage s has been read whole, stage s + 1 has arrived
-        next = codes_of(s + 2);
-        load_scales((s + 1) / kBatch + 1, static_cast<int>((s + 1) % kBatch) % kScaleLoads);
+        // stage s has been read whole, stage s + 1 has arrived
+        sync(std::integral_constant<int, (NS - 2) * kLoads>{});
+        next = codes_of(s + NS);
+        // (with two stages a batch's loads are repeated rather than skipped: all
+        // have arrived before they are read, and the branch costs registers)
+        if (NS == 2 || (s + 1) % kBatch < kScaleLoads)
+            load_scales((s + 1) / kBatch + 1, static_cast<int>((s + 1) % kBatch) % kScaleLoads);
         read_scales(s + 1, sa[1], sb[1]);
         depth(std::integral_constant<int, 3>{}, s);
         keep_scales(s + 1, sa[1], sb[1]);
@@ -494,8 +526,8 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx4_tiles(MatmulArgs g)
     // added to is read 64 rows ahead (4096 x 4096 x 8192 to fp32 88 us, 95 where a
     // row's are read before its store).
     constexpr int kCols = 32 * FN, kPitch = kCols + 8, kLanes = kCols / 4, kTurns = 32 * kLanes / 64;
-    static_assert(FM >= 2 && W * 32 * kPitch * 4 <= sizeof(smem) && kPitch % 16 == 8, "the waves' parts fit the stages");
-    sync();
+    static_assert(W * 32 * kPitch * 4 <= sizeof(smem) && kPitch % 16 == 8, "the waves' parts fit the stages");
+    sync(std::integral_constant<int, 0>{});
     float* mine = reinterpret_cast<float*>(smem) + wave * 32 * kPitch;
     const int64_t col = col0 + wn * kCols + (lane % kLanes) * 4, first = row0 + wm * 32 * FM + lane / kLanes;
     const bool add = g.accumulate != 0;
@@ -510,7 +542,8 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx4_tiles(MatmulArgs g)
     };
     if (add) {
         load_old(0);
-        load_old(1);
+        if constexpr (FM > 1)
+            load_old(1);
     }
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
@@ -708,7 +741,7 @@ hipError_t over_blocks(F kernel, MatmulArgs g, int64_t blocks, unsigned threads,
     return hipSuccess;
 }
 
-template <int T, int WM, int WN, int FM, int FN>
+template <int T, int WM, int WN, int FM, int FN, int NS>
 hipError_t tiles(MatmulArgs g, int32_t parts, float* ws, hipStream_t stream)
 {
     constexpr int BM = 32 * WM * FM, BN = 32 * WN * FN;
@@ -717,7 +750,7 @@ hipError_t tiles(MatmulArgs g, int32_t parts, float* ws, hipStream_t stream)
     if (parts == 1) {
         g.part_blocks = g.nkb;
         g.part_bytes = 0;
-        return over_blocks(k_mx4_tiles<T, WM, WN, FM, FN>, g, int64_t(g.tiles_m) * g.tiles_n, 64 * WM * WN, stream);
+        return over_blocks(k_mx4_tiles<T, WM, WN, FM, FN, NS>, g, int64_t(g.tiles_m) * g.tiles_n, 64 * WM * WN, stream);
     }
     constexpr int64_t kUnit = kBatch * kStageBlocks;
     MatmulArgs p = g;
@@ -726,7 +759,7 @@ hipError_t tiles(MatmulArgs g, int32_t parts, float* ws, hipStream_t stream)
     p.part_bytes = g.m * p.ldo * 4;
     p.out = ws;
     p.accumulate = 0;
-    hipError_t e = over_blocks(k_mx4_tiles<kF32, WM, WN, FM, FN>, p, int64_t(g.tiles_m) * g.tiles_n * parts,
+    hipError_t e = over_blocks(k_mx4_tiles<kF32, WM, WN, FM, FN, NS>, p, int64_t(g.tiles_m) * g.tiles_n * parts,
                                64 * WM * WN, stream);
     const int64_t per_row = p.ldo / 4, most = (int64_t(1) << 30) / per_row < 1 ? 1 : (int64_t(1) << 30) / per_row;
     const RowDiv div = row_div(static_cast<uint32_t>(per_row));
@@ -758,11 +791,21 @@ hipError_t rows_by(const MatmulArgs& g, int32_t nt, hipStream_t stream)
     return nt == 1 ? rows_by<MT, 1>(g, stream) : nt == 2 ? rows_by<MT, 2>(g, stream) : rows_by<MT, 4>(g, stream);
 }
 
+// Two stages of 128 x 128 leave room for another block on the compute unit,
+// four are faster where there is none: 126 x 1628 x 13400 40 us with four, 53 with
+// two (13 blocks); 1024 x 8192 x 8192 57 and 53 (512 blocks).  Eight waves of 64
+// x 32 outputs take 14.0 us for 192 x 4096 x 4096, four of 64 x 64 14.8; of 64 x 128
+// outputs, four of 32 x 64 10.9, two of 64 x 64 14.2.
 template <int T>
 hipError_t tiles(const MatmulArgs& g, const MatmulPlan& plan, float* ws, hipStream_t stream)
 {
-    return plan.form == MatmulPlan::kTiles256 ? tiles<T, 2, 4, 4, 2>(g, 1, ws, stream)
-                                              : tiles<T, 2, 2, 2, 2>(g, plan.parts, ws, stream);
+    switch (plan.form) {
+    case MatmulPlan::kTiles64: return tiles<T, 2, 2, 1, 2, 4>(g, plan.parts, ws, stream);
+    case MatmulPlan::kTiles128:
+        return tile_blocks(g.m, g.n, plan.form) * plan.parts <= kUnits ? tiles<T, 2, 4, 2, 1, 4>(g, plan.parts, ws, stream)
+                                                                 : tiles<T, 2, 2, 2, 2, 2>(g, plan.parts, ws, stream);
+    default: return tiles<T, 2, 4, 4, 2, 2>(g, 1, ws, stream);
+    }
 }
 
 hipError_t product(const MatmulArgs& g, const MatmulPlan& plan, float* ws, hipStream_t stream)

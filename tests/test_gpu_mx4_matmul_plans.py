@@ -41,7 +41,19 @@ def test_ragged_tiles(m, n, k, dtype):
     assert (out[:, n:] == -3.0).all()
 
 
-@pytest.mark.parametrize("m,n,k", [(300, 6000, 600), (1000, 1030, 9001), (5001, 2003, 257)])
+# tiles of each size, with 2 and 4 stages in LDS, in one part and in several
+@pytest.mark.parametrize("m,n,k", [(562, 3199, 197), (519, 1694, 12261), (81, 2668, 9178), (164, 466, 13001),
+                                   (588, 4686, 426), (998, 3709, 1993), (355, 1296, 15040), (128, 2726, 14204),
+                                   (839, 5586, 283), (2308, 5034, 1066)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("accumulate", [0, 1])
+def test_every_tile(m, n, k, dtype, accumulate):
+    out, want, _, _ = case(m, n, k, dtype, accumulate, m + n + k)
+    assert torch.equal(out[:, :n].cpu(), want.to(out.dtype))
+    assert (out[:, n:] == -3.0).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(300, 6000, 600), (1000, 1030, 9001), (998, 3709, 1993), (5001, 2003, 257)])
 def test_nan_blocks_in_tiles(m, n, k):
     rng = np.random.default_rng(m)
     a, b = operand(m, k, rng, 127, 127, 1), operand(n, k, rng, 127, 127, 0)
@@ -56,7 +68,7 @@ def test_nan_blocks_in_tiles(m, n, k):
     assert torch.equal(torch.nan_to_num(out[:, :n].cpu().double(), nan=1e30), torch.nan_to_num(want, nan=1e30))
 
 
-@pytest.mark.parametrize("m,n,k", [(140, 9001, 700), (1030, 1000, 9000)])
+@pytest.mark.parametrize("m,n,k", [(140, 9001, 700), (1030, 1000, 9000), (998, 3709, 1993)])
 def test_extreme_scales_in_tiles(m, n, k):
     """Bytes 1 and 253 against their opposites: 2^-126 * 2^126 = 1."""
     rng = np.random.default_rng(n)
@@ -79,7 +91,7 @@ def test_tiles_in_many_launches():
         assert torch.equal(out[:, :want.shape[1]].cpu().double(), want)
 
 
-@pytest.mark.parametrize("m,n,k", [(700, 900, 9001), (1000, 1030, 9001), (512, 512, 16390)])
+@pytest.mark.parametrize("m,n,k", [(700, 900, 9001), (200, 1000, 20000), (355, 1296, 15040), (512, 512, 16390)])
 def test_split_sums_on_two_streams_at_once(m, n, k):
     """Two products at once, each with a workspace of its own."""
     assert uq.uq_mx4_matmul_workspace_bytes(m, n, k) > 256  # k is split
@@ -103,7 +115,7 @@ def test_split_sums_on_two_streams_at_once(m, n, k):
 
 
 @pytest.mark.parametrize("m,n,k", [(1, 300, 700), (40, 8200, 512), (300, 200, 4096), (700, 900, 9001), (300, 5001, 600),
-                                   (5001, 2003, 257)])
+                                   (998, 3709, 1993), (5001, 2003, 257)])
 @pytest.mark.parametrize("accumulate", [0, 1])
 def test_replays(m, n, k, accumulate):
     """Captured once; the replays read the operands as they then are, between
