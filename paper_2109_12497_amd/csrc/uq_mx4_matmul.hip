@@ -105,15 +105,17 @@ double rows_ns(const MatmulPlan& plan, int64_t m, int64_t n, int64_t k)
     return 1800.0 + rounds * (0.02 * read + 220.0 * plan.mt * plan.nt);
 }
 
-MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
+// One form for the whole product; *ns is the time it takes.
+MatmulPlan one_plan(int64_t m, int64_t n, int64_t k, double* ns)
 {
     // 64 x 4096 x 4096 8.9 us as few rows, 10.4 in tiles; 64 x 28672 x 8192 58 and
     // 31; 256 x 1000 x 20000 22 and 16 (eight parts)
     MatmulPlan best = rows_plan(m, n);
+    double& least = *ns;
+    least = rows_ns(best, m, n, k);
     if (k == 0)
         return best;
     const int64_t stages = (k + 255) / 256, batches = (stages + kBatch - 1) / kBatch;
-    double least = rows_ns(best, m, n, k);
     // parts of more outputs than this never pay, and bound the workspace (512 MB)
     const int32_t most = m * n <= kMostParted ? 8 : 1;
     for (int32_t parts = 1; parts <= most && parts <= batches; parts *= 2) {
@@ -123,15 +125,58 @@ MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k)
             // us in two, 16.5 in one of 128 x 128
             if (form == MatmulPlan::kTiles64 && tile_blocks(m, n, form) * parts > kUnits)
                 continue;
-            const double ns = tiles_ns(m, n, deep, parts, form);
-            if (ns < least) {
-                least = ns;
+            const double t = tiles_ns(m, n, deep, parts, form);
+            if (t < least) {
+                least = t;
                 best = {form, parts, 0, 0};
             }
         }
     }
-    if (tiles_ns(m, n, stages, 1, MatmulPlan::kTiles256) < least)
+    const double t = tiles_ns(m, n, stages, 1, MatmulPlan::kTiles256);
+    if (t < least) {
+        least = t;
         best = {MatmulPlan::kTiles256, 1, 0, 0};
+    }
+    return best;
+}
+
+// A product in one form, or its first rows (or columns) in tiles that fill
+// whole rounds and the others in a form of their own.
+struct MatmulSplit {
+    MatmulPlan first, rest;
+    int64_t m, n;  // of the first
+};
+
+// 2304 x 8497 x 13601 in 306 tiles of 256 x 256 takes two rounds for a round
+// and a fifth, 216 us; 252 tiles and then 1329 columns 182.  2112 x 7854 x 7168 98.6
+// and 71.9 us.
+MatmulSplit matmul_plan(int64_t m, int64_t n, int64_t k)
+{
+    double least;
+    MatmulSplit best = {one_plan(m, n, k, &least), {}, m, n};
+    if (m == 0 || n == 0 || k == 0)
+        return best;
+    constexpr double kLaunch = 2000.0;  // the second launch
+    const int64_t stages = (k + 255) / 256;
+    for (const auto form : {MatmulPlan::kTiles128, MatmulPlan::kTiles256}) {
+        const int64_t side = form == MatmulPlan::kTiles128 ? 128 : 256;
+        const int64_t round = form == MatmulPlan::kTiles128 ? 2 * kUnits : kUnits;
+        const int64_t down = (m + side - 1) / side, across = (n + side - 1) / side;
+        const int64_t full = down * across / round * round;  // tiles in whole rounds
+        for (const bool by_rows : {false, true}) {
+            const int64_t lines = full / (by_rows ? across : down);
+            if (lines == 0 || lines >= (by_rows ? down : across))
+                continue;
+            const int64_t m1 = by_rows ? lines * side : m, n1 = by_rows ? n : lines * side;
+            double rest;
+            const MatmulPlan plan = one_plan(by_rows ? m - m1 : m, by_rows ? n : n - n1, k, &rest);
+            const double t = tiles_ns(m1, n1, stages, 1, form) + rest + kLaunch;
+            if (t < least) {
+                least = t;
+                best = {{form, 1, 0, 0}, plan, m1, n1};
+            }
+        }
+    }
     return best;
 }
 
@@ -823,10 +868,17 @@ hipError_t product(const MatmulArgs& g, const MatmulPlan& plan, float* ws, hipSt
 
 }  // namespace
 
+static size_t parts_bytes(const MatmulPlan& plan, int64_t m, int64_t n)
+{
+    return plan.parts > 1 ? align256(static_cast<size_t>(plan.parts) * m * ((n + 3) / 4 * 4) * sizeof(float)) : 256;
+}
+
 size_t mx4_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k)
 {
-    const MatmulPlan plan = matmul_plan(m, n, k);
-    return plan.parts > 1 ? align256(static_cast<size_t>(plan.parts) * m * ((n + 3) / 4 * 4) * sizeof(float)) : 256;
+    const MatmulSplit s = matmul_plan(m, n, k);
+    const size_t first = parts_bytes(s.first, s.m, s.n);
+    const size_t rest = s.m < m ? parts_bytes(s.rest, m - s.m, n) : s.n < n ? parts_bytes(s.rest, m, n - s.n) : 0;
+    return first > rest ? first : rest;
 }
 
 hipError_t launch_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* as, int64_t ldas, const uint8_t* b,
@@ -836,12 +888,29 @@ hipError_t launch_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* as, i
     if (m == 0 || n == 0)
         return hipSuccess;
     constexpr int64_t kMostLd = 1 << 23;  // a tile's rows lie within a buffer's 2^31 bytes
-    MatmulPlan plan = matmul_plan(m, n, k);
-    const MatmulArgs g = {a, as, b, bs, lda, ldas, ldb, ldbs, m, n, (k + 31) / 32, out, ldo, type, accumulate,
-                          0, 0, 0, 0, 0};
-    if (plan.form != MatmulPlan::kRows && (lda > kMostLd || ldb > kMostLd || ldas > kMostLd || ldbs > kMostLd))
-        plan = rows_plan(m, n);
-    return product(g, plan, static_cast<float*>(ws), stream);
+    MatmulArgs g = {a, as, b, bs, lda, ldas, ldb, ldbs, m, n, (k + 31) / 32, out, ldo, type, accumulate,
+                    0, 0, 0, 0, 0};
+    if (lda > kMostLd || ldb > kMostLd || ldas > kMostLd || ldbs > kMostLd)
+        return product(g, rows_plan(m, n), nullptr, stream);
+    const MatmulSplit s = matmul_plan(m, n, k);
+    g.m = s.m;
+    g.n = s.n;
+    const hipError_t e = product(g, s.first, static_cast<float*>(ws), stream);
+    if (e != hipSuccess || (s.m == m && s.n == n))
+        return e;
+    const int64_t size = type == kF32 ? 4 : 2;
+    if (s.m < m) {
+        g.m = m - s.m;
+        g.a += s.m * lda;
+        g.as += s.m * ldas;
+        g.out = static_cast<char*>(out) + s.m * ldo * size;
+    } else {
+        g.n = n - s.n;
+        g.b += s.n * ldb;
+        g.bs += s.n * ldbs;
+        g.out = static_cast<char*>(out) + s.n * size;
+    }
+    return product(g, s.rest, static_cast<float*>(ws), stream);
 }
 
 }  // namespace uq

@@ -53,7 +53,28 @@ def test_every_tile(m, n, k, dtype, accumulate):
     assert (out[:, n:] == -3.0).all()
 
 
-@pytest.mark.parametrize("m,n,k", [(300, 6000, 600), (1000, 1030, 9001), (998, 3709, 1993), (5001, 2003, 257)])
+# tiles that fill whole rounds, and the last rows or columns in another form
+@pytest.mark.parametrize("m,n,k", [(5911, 1325, 16), (674, 11181, 17), (10760, 1624, 16), (6854, 2483, 33),
+                                   (9576, 1726, 100), (6736, 2671, 16), (1777, 10176, 16), (8022, 2068, 161),
+                                   (3971, 4352, 262), (4103, 4001, 513)])
+@pytest.mark.parametrize("dtype,accumulate", [("fp32", 1), ("bf16", 0), ("fp16", 1)])
+def test_whole_rounds_and_a_rest(m, n, k, dtype, accumulate):
+    out, want, _, _ = case(m, n, k, dtype, accumulate, m + n + k)
+    assert torch.equal(out[:, :n].cpu(), want.to(out.dtype))
+    assert (out[:, n:] == -3.0).all()
+
+
+def test_whole_rounds_and_a_split_rest():
+    """The last rows' k in parts, which need the workspace."""
+    m, n, k = 8400, 2000, 8192
+    assert uq.uq_mx4_matmul_workspace_bytes(m, n, k) > 256
+    out, want, _, _ = case(m, n, k, "fp32", 1, 6)
+    assert torch.equal(out[:, :n].cpu().double(), want)
+    assert (out[:, n:] == -3.0).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(300, 6000, 600), (1000, 1030, 9001), (998, 3709, 1993), (5001, 2003, 257),
+                                   (3971, 4352, 262)])
 def test_nan_blocks_in_tiles(m, n, k):
     rng = np.random.default_rng(m)
     a, b = operand(m, k, rng, 127, 127, 1), operand(n, k, rng, 127, 127, 0)
@@ -115,7 +136,7 @@ def test_split_sums_on_two_streams_at_once(m, n, k):
 
 
 @pytest.mark.parametrize("m,n,k", [(1, 300, 700), (40, 8200, 512), (300, 200, 4096), (700, 900, 9001), (300, 5001, 600),
-                                   (998, 3709, 1993), (5001, 2003, 257)])
+                                   (998, 3709, 1993), (5001, 2003, 257), (3971, 4352, 262)])
 @pytest.mark.parametrize("accumulate", [0, 1])
 def test_replays(m, n, k, accumulate):
     """Captured once; the replays read the operands as they then are, between
