@@ -73,14 +73,15 @@ double tiles_ns(int64_t m, int64_t n, int64_t stages, int64_t parts, MatmulPlan:
 // and 23.6 with 3, 4 and 1; 32 x 4096 x 4096 6.6 with 1, 7.6, 8.9 and 10.0 with
 // 2, 3 and 4; 32 x 28672 x 8192 38.9 with 4 (448), 48.3, 49.0 and 56.7 with 3, 2
 // and 1.  Three beside one fragment of a never were the best (16 x 10001 x 5003
-// 14.8, with 1 11.5).
+// 14.8, with 1 11.5), and four beside four, which do not fit the registers, nowhere
+// by more than 3% before tiles.
 MatmulPlan rows_plan(int64_t m, int64_t n)
 {
     MatmulPlan best = {MatmulPlan::kRows, 1, m <= 16 ? 1 : m <= 32 ? 2 : m <= 48 ? 3 : 4, 1};
     const int64_t down = (m + 16 * best.mt - 1) / (16 * best.mt), a = m < 16 * best.mt ? m : 16 * best.mt;
     double least = 0.0;
     for (int32_t nt = 1; nt <= 4; ++nt) {
-        if (nt == 3 && best.mt == 1)
+        if ((nt == 3 && best.mt == 1) || (nt == 4 && best.mt == 4))
             continue;
         const int64_t blocks = down * ((n + 16 * nt - 1) / (16 * nt));
         const double rows = static_cast<double>((blocks + 255) / 256) * (0.5 * static_cast<double>(a) + 16.0 * nt);
@@ -830,10 +831,16 @@ hipError_t rows_by(MatmulArgs g, hipStream_t stream)
 template <int MT>
 hipError_t rows_by(const MatmulArgs& g, int32_t nt, hipStream_t stream)
 {
+    if (nt == 1)
+        return rows_by<MT, 1>(g, stream);
+    if (nt == 2)
+        return rows_by<MT, 2>(g, stream);
     if constexpr (MT > 1)
         if (nt == 3)
             return rows_by<MT, 3>(g, stream);
-    return nt == 1 ? rows_by<MT, 1>(g, stream) : nt == 2 ? rows_by<MT, 2>(g, stream) : rows_by<MT, 4>(g, stream);
+    if constexpr (MT < 4)
+        return rows_by<MT, 4>(g, stream);
+    return hipErrorInvalidValue;  // rows_plan gives no other
 }
 
 // Two stages of 128 x 128 leave room for another block on the compute unit,
