@@ -217,17 +217,30 @@ __device__ __forceinline__ f32x4 values(Four<T> x)
 }
 
 // Columns col .. col + 3 (a multiple of 4) of the row that starts at `row`, of
-// n; `old` is what load_four read there before.
-template <int T>
+// n; `old` is what load_four read there before.  PAST, past: nontemporally.
+template <int T, bool PAST>
 __device__ __forceinline__ Four<T> load_four(const void* out, int64_t row, int64_t col, int64_t n)
 {
     using Element = std::conditional_t<T == kF32, float, uint16_t>;
-    return col + 4 > n ? Four<T>{} : *reinterpret_cast<const Four<T>*>(static_cast<const Element*>(out) + row + col);
+    const auto* at = reinterpret_cast<const Four<T>*>(static_cast<const Element*>(out) + row + col);
+    return col + 4 > n ? Four<T>{} : PAST ? __builtin_nontemporal_load(at) : *at;
+}
+
+template <typename V>
+__device__ __forceinline__ void store_past(bool past, V v, V* at)
+{
+    if (past) {  // empty statements keep the compiler from merging the stores into a plain one
+        asm volatile("");
+        __builtin_nontemporal_store(v, at);
+        asm volatile("");
+    } else {
+        *at = v;
+    }
 }
 
 template <int T>
 __device__ __forceinline__ void store_four(void* out, int64_t row, int64_t col, int64_t n, f32x4 v, bool accumulate,
-                                           Four<T> old)
+                                           Four<T> old, bool past)
 {
     if (col + 4 > n) {
 #pragma unroll
@@ -239,17 +252,17 @@ __device__ __forceinline__ void store_four(void* out, int64_t row, int64_t col, 
     if (accumulate)
         v += values<T>(old);
     if constexpr (T == kF32) {
-        *reinterpret_cast<f32x4*>(static_cast<float*>(out) + row + col) = v;
+        store_past(past, v, reinterpret_cast<f32x4*>(static_cast<float*>(out) + row + col));
     } else {
         u32x2* o = reinterpret_cast<u32x2*>(static_cast<uint16_t*>(out) + row + col);
         if constexpr (T == kBF16) {
             const bf16x2 a = {static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1])};
             const bf16x2 b = {static_cast<__bf16>(v[2]), static_cast<__bf16>(v[3])};
-            *o = u32x2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
+            store_past(past, u32x2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)}, o);
         } else {
             const f16x2 a = {static_cast<_Float16>(v[0]), static_cast<_Float16>(v[1])};
             const f16x2 b = {static_cast<_Float16>(v[2]), static_cast<_Float16>(v[3])};
-            *o = u32x2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
+            store_past(past, u32x2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)}, o);
         }
     }
 }
@@ -295,6 +308,7 @@ struct MatmulArgs {
     int64_t part_blocks;  // blocks along k of a part (all of them: one part)
     int64_t part_bytes;   // between the parts' outputs
     int32_t first;        // the launch's first block
+    bool past;            // tiles' outputs are stored nontemporally
 };
 
 // Block -> tile.  Blocks go to the eight XCDs in turn, and each XCD has its
@@ -578,12 +592,16 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx4_tiles(MatmulArgs g)
     const int64_t col = col0 + wn * kCols + (lane % kLanes) * 4, first = row0 + wm * 32 * FM + lane / kLanes;
     const bool add = g.accumulate != 0;
     Four<T> old[3][kTurns];
+    // Large tiles read them nontemporally (8192^3 added to bf16, outputs in turn,
+    // 303 us, 326 otherwise; 4096 x 4096 x 8192 to fp32 92 either way), small ones not
+    // (1000 x 3000 x 700 11.7 and 10.5).
+    constexpr bool kPast = BM * BN >= 256 * 256;
     const auto load_old = [&](int i) {
 #pragma unroll
         for (int r = 0; r < kTurns; ++r) {
             const int64_t row = first + 32 * i + r * (64 / kLanes);
             if (row < g.m)
-                old[i % 3][r] = load_four<T>(out, row * g.ldo, col, g.n);
+                old[i % 3][r] = load_four<T, kPast>(out, row * g.ldo, col, g.n);
         }
     };
     if (add) {
@@ -607,7 +625,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx4_tiles(MatmulArgs g)
             const f32x4 v = *reinterpret_cast<const f32x4*>(mine + (at + lane / kLanes) * kPitch + (lane % kLanes) * 4);
             const int64_t row = first + 32 * i + at;
             if (row < g.m)
-                store_four<T>(out, row * g.ldo, col, g.n, v, add, old[i % 3][r]);
+                store_four<T>(out, row * g.ldo, col, g.n, v, add, old[i % 3][r], g.past);
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -624,11 +642,11 @@ __global__ __launch_bounds__(kBlock) void k_mx4_join(const float* parts, int32_t
         return;
     const uint32_t in = div_row(u, div);
     const int64_t row = row0 + in, col = int64_t(u - in * div.n) * 4;
-    const Four<T> old = accumulate != 0 ? load_four<T>(out, row * ldo, col, n) : Four<T>{};
+    const Four<T> old = accumulate != 0 ? load_four<T, false>(out, row * ldo, col, n) : Four<T>{};
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int32_t c = 0; c < count; ++c)
         v += *reinterpret_cast<const f32x4*>(parts + (c * m + row) * ldp + col);
-    store_four<T>(out, row * ldo, col, n, v, accumulate != 0, old);
+    store_four<T>(out, row * ldo, col, n, v, accumulate != 0, old, false);
 }
 
 // ---------------------------------------------------------------------------
@@ -880,6 +898,12 @@ hipError_t product(const MatmulArgs& g, const MatmulPlan& plan, float* ws, hipSt
 
 }  // namespace
 
+// Outputs from half the Infinity Cache's size on pass it by: 8192 x 4096 x 4096
+// added to fp32 (134 MB), three outputs in turn, 125 us, 141 otherwise (one output
+// each time 124 and 110); 4096 x 4096 x 8192 (67 MB) 94 either way, and 94 and
+// 89; 8192^3 to bf16 (134 MB), outputs in turn, 277 and 294.
+constexpr double kPastBytes = 128.0 * (1 << 20);
+
 static size_t parts_bytes(const MatmulPlan& plan, int64_t m, int64_t n)
 {
     return plan.parts > 1 ? align256(static_cast<size_t>(plan.parts) * m * ((n + 3) / 4 * 4) * sizeof(float)) : 256;
@@ -900,8 +924,9 @@ hipError_t launch_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* as, i
     if (m == 0 || n == 0)
         return hipSuccess;
     constexpr int64_t kMostLd = 1 << 23;  // a tile's rows lie within a buffer's 2^31 bytes
+    const int64_t size = type == kF32 ? 4 : 2;
     MatmulArgs g = {a, as, b, bs, lda, ldas, ldb, ldbs, m, n, (k + 31) / 32, out, ldo, type, accumulate,
-                    0, 0, 0, 0, 0};
+                    0, 0, 0, 0, 0, static_cast<double>(m) * static_cast<double>(n * size) >= kPastBytes};
     if (lda > kMostLd || ldb > kMostLd || ldas > kMostLd || ldbs > kMostLd)
         return product(g, rows_plan(m, n), nullptr, stream);
     const MatmulSplit s = matmul_plan(m, n, k);
@@ -910,7 +935,6 @@ hipError_t launch_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* as, i
     const hipError_t e = product(g, s.first, static_cast<float*>(ws), stream);
     if (e != hipSuccess || (s.m == m && s.n == n))
         return e;
-    const int64_t size = type == kF32 ? 4 : 2;
     if (s.m < m) {
         g.m = m - s.m;
         g.a += s.m * lda;

@@ -204,3 +204,14 @@ def test_layer_that_grows_its_workspace_on_a_given_stream():
         y = layer.forward(x, stream=stream)
         torch.cuda.synchronize()
         assert torch.equal(y.cpu().double(), want)
+
+
+@pytest.mark.parametrize("m,n,k,dtype", [(5901, 5703, 64, "fp32"), (8201, 8190, 40, "bf16"), (65537, 1030, 300, "fp16"),
+                                         (33001, 1025, 65, "fp32")])
+@pytest.mark.parametrize("accumulate", [0, 1])
+def test_outputs_that_pass_the_cache_by(m, n, k, dtype, accumulate):
+    """128 MiB of outputs and more."""
+    assert m * n * (4 if dtype == "fp32" else 2) >= 128 << 20
+    out, want, _, _ = case(m, n, k, dtype, accumulate, m + n + k)
+    assert torch.equal(out[:, :n].cpu(), want.to(out.dtype))
+    assert (out[:, n:] == -3.0).all()
