@@ -400,7 +400,7 @@ struct Operand {
 // instruction t = 0..3: any order of the blocks along k gives the same
 // products as long as both operands keep to it, and in this one a lane's four
 // scale bytes are one dword.
-//   What bounds it, 8192^3 to bf16 on one MI355X: 264 us, 4160 TFLOP/s.  The
+//   What bounds it, 8192^3 to bf16 on one MI355X: 261 us, 4210 TFLOP/s.  The
 // card lowers its clock by the data: on zeros the same instructions take 187
 // us (5890), and matrix instructions alone reach 6540 on random codes and 9000
 // on zeros.  The rest is the loads into LDS (without them, on random codes, 15%
