@@ -7,7 +7,7 @@ to the current stream of the device the buffers are on, or to the one given.
 """
 from __future__ import annotations
 
-import contextlib
+import functools
 
 import torch
 
@@ -32,11 +32,18 @@ def _settle(device) -> None:
         torch.cuda.current_stream(device).synchronize()
 
 
-def _on(stream: int | None):
-    """torch's current stream set to a raw handle (None or the current one: as it is)."""
-    if stream is None or stream == _stream(None):
-        return contextlib.nullcontext()
-    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream())
+@functools.lru_cache(maxsize=256)
+def _layer_workspace_bytes(tokens: int, inputs: int, outputs: int, train: bool) -> int:
+    """What the products of any number of rows up to `tokens` need at most.
+    Fewer rows can need more: k is split where tiles are few.  (A plan takes
+    about 1.5 us of the host, so 8192 tokens about 40 ms, once for a shape.)"""
+    most = 0
+    for rows in range(1, tokens + 1):
+        most = max(most, uq_mx4_matmul_workspace_bytes(rows, outputs, inputs))
+        if train:
+            most = max(most, uq_mx4_matmul_workspace_bytes(rows, inputs, outputs),
+                       uq_mx4_matmul_workspace_bytes(outputs, inputs, rows))
+    return most
 
 
 def _check_matrix(t, rows: int, cols: int, device) -> None:
@@ -85,7 +92,8 @@ class Mx4Linear:
     quantised x and w, and returns (dx, dw); with accumulate=True dw is added to
     what the buffer holds.  y, dx and dw are views of the layer's own buffers (y
     and dx of `dtype`, dw in binary32) and stay until the next call that
-    writes them.
+    writes them.  Calls allocate nothing: the workspace is sized once, for the
+    number of rows that needs the most.
     """
 
     def __init__(self, tokens: int, inputs: int, outputs: int, dtype=torch.float32, device="cuda", train: bool = True):
@@ -102,24 +110,10 @@ class Mx4Linear:
             self.dy_t = Codes(outputs, tokens, dev)
             self.dx = torch.zeros((tokens, round_up(inputs, 8)), dtype=dtype, device=dev)
             self.dw = torch.zeros((outputs, round_up(inputs, 4)), dtype=torch.float32, device=dev)
-        self.ws, self._kept = torch.empty(256, dtype=torch.uint8, device=dev), []
-        self._reserve(tokens)
+        # for every number of rows, so that no call allocates and a captured graph's stays where it is
+        self.ws = torch.empty(_layer_workspace_bytes(tokens, inputs, outputs, train), dtype=torch.uint8, device=dev)
         self.rows = 0  # of the last forward
         _settle(dev)
-
-    def _reserve(self, rows: int, stream: int | None = None) -> None:
-        """Workspace for the products of `rows` tokens (fewer tokens can need
-        more: k is split where tiles are few), kept for later calls.  It is
-        allocated on the stream that will use it, and not cleared: what ran on
-        that memory before, or a fill on another stream, would race."""
-        need = [uq_mx4_matmul_workspace_bytes(rows, self.outputs, self.inputs)]
-        if self.train:
-            need += [uq_mx4_matmul_workspace_bytes(rows, self.inputs, self.outputs),
-                     uq_mx4_matmul_workspace_bytes(self.outputs, self.inputs, rows)]
-        if max(need) > self.ws.numel():
-            self._kept.append(self.ws)  # a captured graph may still use it
-            with _on(stream):
-                self.ws = torch.empty(max(need), dtype=torch.uint8, device=self.device)
 
     def _matmul(self, a: Codes, b: Codes, m: int, n: int, k: int, out, accumulate: bool, stream) -> None:
         uq_mx4_matmul(*a.args(), *b.args(), m, n, k, TYPES[out.dtype], out, out.stride(0), int(accumulate), self.ws,
@@ -135,7 +129,6 @@ class Mx4Linear:
         assert rows <= self.tokens
         _check_matrix(x, rows, self.inputs, self.device)
         stream = _stream(stream)  # resolved once for the calls
-        self._reserve(rows, stream)
         self.rows = rows
         quantize(x, self.x, self.x_t if self.train else None, stream=stream)
         self._matmul(self.x, self.w, rows, self.outputs, self.inputs, self.y, False, stream)
