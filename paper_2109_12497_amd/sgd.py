@@ -46,6 +46,11 @@ from .step import Step
 
 MX4 = "mx4"  # in place of a scale set: microscaled 4-bit codes
 
+# A run aggregates with the seeds seed * 1_000_003 + t.  What rounds gradients
+# counts up from here instead: with a seed of both, the words that rounded the
+# residuals would round the gradients formed from them again.
+GRADIENT_SEEDS = 1 << 63
+
 
 @dataclass
 class LeastSquares:
@@ -163,9 +168,9 @@ class Mx4Aggregate:
 class Mx4Gradients:
     """shard_gradients through a layer of one output: y = A_m theta forward and
     A_m^T (y - b_m) / rows backward, on 4-bit operands (theta and A_m rounded to
-    the nearest, the residuals stochastically)."""
+    the nearest, the residuals stochastically, by the seeds after `seed`)."""
 
-    def __init__(self, p: LeastSquares, seed: int = 0):
+    def __init__(self, p: LeastSquares, seed: int = GRADIENT_SEEDS):
         M, rows, n = p.A.shape
         self.layer = Mx4Linear(rows, n, 1, device=p.A.device)
         self.x = torch.zeros((M, rows, -(-n // 4) * 4), dtype=torch.float32, device=p.A.device)
@@ -263,7 +268,7 @@ def main() -> int:
             return Mx4Aggregate(p.n, p.M, dev)
         return mean_aggregate if scales is None else QuantisedAggregate(p.n, p.M, scales, dev)
 
-    gradients = Mx4Gradients(p, args.seed) if args.gradients == MX4 else shard_gradients
+    gradients = Mx4Gradients(p, GRADIENT_SEEDS + (args.seed << 32)) if args.gradients == MX4 else shard_gradients
     table = convergence_table(p, make, args.T, configs={**CONFIGS, MX4: MX4}, gradients=gradients)
     print(json.dumps(dict(n=p.n, M=p.M, rows=args.rows, T=args.T, gradients=args.gradients, L=p.L, R=p.R, W_max=p.W_max, f_star=p.f_star,
                           table=table), indent=1))

@@ -48,3 +48,47 @@ def test_no_bound_for_other_gradients(problem):
         (row,) = sgd.convergence_table(problem, make, T=3, seeds=(0,), configs=configs, gradients=biased).values()
         assert "bound" not in row and "sigma2_bound" not in row
         assert all(np.isfinite(v) for v in row.values()) and set(row) >= {"eta", "gap_avg", "gap_tail_fixed_step"}
+
+
+def test_gradients_and_aggregation_take_separate_seeds(monkeypatch, capsys):
+    """Every seed that the command's layer and its aggregators are given: none twice
+    within one, none of both."""
+    rounded, aggregated = [], []
+
+    class Layer:
+        def __init__(self, tokens, inputs, outputs, device):
+            self.shape = tokens, inputs
+
+        def load(self, w):
+            pass
+
+        def forward(self, x):
+            return torch.zeros(self.shape[0], 1)
+
+        def backward(self, dy, seed):
+            rounded.append(seed)
+            return None, torch.zeros(1, self.shape[1])
+
+    def aggregator(*a):
+        def run(grads, d, seed):
+            aggregated.append(seed)
+            return grads[:, :d].mean(0)
+        return run
+
+    make_problem = sgd.make_problem
+    monkeypatch.setattr(sgd, "Mx4Linear", Layer)
+    monkeypatch.setattr(sgd, "QuantisedAggregate", aggregator)
+    monkeypatch.setattr(sgd, "Mx4Aggregate", aggregator)
+    monkeypatch.setattr(sgd, "make_problem", lambda n, M, rows, seed, device: make_problem(n=n, M=M, rows=rows, seed=seed))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    T, M, seeds, settings = 5, 2, 3, len(sgd.CONFIGS) + 1
+    monkeypatch.setattr("sys.argv", ["sgd", "--n", "8", "--M", str(M), "--rows", "16", "--T", str(T), "--gradients", "mx4"])
+    assert sgd.main() == 0
+    assert len(rounded) == settings * seeds * 2 * T * M and len(set(rounded)) == len(rounded)
+    assert len(aggregated) == (settings - 1) * seeds * 2 * T and len(set(aggregated)) == seeds * T
+    assert not set(rounded) & set(aggregated)
+    assert all(0 <= s < 1 << 64 for s in rounded + aggregated)
+    del rounded[:]
+    p = make_problem(n=8, M=M, rows=16, seed=1)
+    sgd.Mx4Gradients(p)(p, torch.zeros(8, dtype=torch.float64), torch.zeros(M, 8))
+    assert min(rounded) >= sgd.GRADIENT_SEEDS > max(aggregated)
