@@ -445,6 +445,10 @@ int uq_scatter_into(const float* vals, const uint32_t* sel, int64_t K, float* ou
  * r < floor((q - l) * 2^32), with the 32-bit uniform word r of row i ("worker"
  * i) at column j as above (the arithmetic contract; key = seed).  The field's
  * sign is x's sign bit, also where the magnitude becomes 0.
+ *   A word depends on the seed, the row and the column alone.  A value that is
+ * formed from stochastic codes and rounded again needs another seed, or its
+ * rounding is not independent of it and the result is biased: each layer of a
+ * backward pass, and the step on its gradients, takes a seed of its own.
  * ------------------------------------------------------------------------ */
 
 /* Element types of matrices. */

@@ -90,7 +90,11 @@ class Mx4Linear:
     the transposed codes of x for dw.  backward(dy, seed) rounds dy
     stochastically, so that both gradients are without bias given the
     quantised x and w, and returns (dx, dw); with accumulate=True dw is added to
-    what the buffer holds.  y, dx and dw are views of the layer's own buffers (y
+    what the buffer holds.  The uniform words are those of (seed, row, column)
+    alone: every layer and every step needs a seed of its own (step * layers +
+    layer, say), and so does a Mx4Step or Step on the gradients.  Where one seed
+    rounds a layer's dy and then the dy formed from it, the second rounding
+    depends on what it rounds and the chain is biased.  y, dx and dw are views of the layer's own buffers (y
     and dx of `dtype`, dw in binary32) and stay until the next call that
     writes them.  Calls allocate nothing: the workspace is sized once, for the
     number of rows that needs the most.
