@@ -537,8 +537,8 @@ int uq_mx4_shared_scale(const float* g, int64_t d, int32_t rows, int64_t ldg, in
  *   sum          [d] int32 (written, or read and written), in half units of
  *                the block's scale; 0 is added where the byte is 255
  *   M, out       NULL: no mean (M is then ignored); else out [d] fp32
- *                (written): RN32(sum_i * RN32(RN32(1 / M) * 2^(e - 1))), NaN
- *                where the byte is 255; M >= 1, 12 * M < 2^31
+ *                (written): RN32(sum_i * 2^(e - 1) / M), rounded once, NaN where
+ *                the byte is 255; M >= 1, 12 * M < 2^31
  */
 int uq_mx4_quantize_sum(const float* g, int64_t d, int32_t rows, int64_t ldg, int32_t worker0, const uint8_t* scales,
                         uint64_t seed, int32_t accumulate, int32_t* sum, int32_t M, float* out, void* stream);

@@ -106,12 +106,12 @@ def quantize_sum(g: np.ndarray, d: int, scale_bytes: np.ndarray, seed: int, work
 
 
 def mean(total: np.ndarray, scale_bytes: np.ndarray, M: int) -> np.ndarray:
-    """RN32(sum * RN32(RN32(1 / M) * 2^(e - 1))), NaN for byte 255."""
+    """RN32(sum * 2^(e - 1) / M), NaN for byte 255: the quotient of integers below
+    2^31 in 64 bits, which rounds to the binary32 number that the exact one does."""
     b = np.repeat(scale_bytes.astype(np.int64), 32)[:total.size]
-    inv = np.float32(1.0 / M)
-    half = (2.0 ** (np.where((b == 255) | (b < 1), 1, b) - 128.0)).astype(np.float32)
+    half = 2.0 ** (np.where((b == 255) | (b < 1), 1, b) - 128.0)
     with np.errstate(over="ignore"):
-        out = total.astype(np.float32) * (inv * half).astype(np.float32)
+        out = (total.astype(np.float64) / M * half).astype(np.float32)
     return np.where(b == 255, np.float32(np.nan), out).astype(np.float32)
 
 

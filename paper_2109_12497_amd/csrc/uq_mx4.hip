@@ -418,13 +418,29 @@ __global__ __launch_bounds__(kBlock) void k_mx4_shared(const float* g, int64_t d
     }
 }
 
-// 2^(e - 1) / M as one binary32 factor (rounded once; NaN for the NaN byte).
-__device__ __forceinline__ float mx4_mean_factor(uint32_t byte, float inv_m)
+// What the mean divides by: the workers and RN64 of their reciprocal.
+struct Mx4Mean {
+    double m, inv_m;
+};
+
+// sum * 2^(e - 1) / M, rounded to binary32 once (NaN for the NaN byte): the
+// quotient in binary64, corrected by its remainder so that it is exact where 64
+// bits hold it, then an exact power of two.  Other quotients of these integers
+// are further from every midpoint of binary32 than binary64 is off (1 / (M j) of
+// themselves for a midpoint of 25 bits j, above 2^-52.5 while 12 M < 2^31).  In
+// binary32, with 2^(e - 1) / M as one factor, the mean was off by up to a whole step
+// for M that are no powers of two, half a step more than the format costs; the
+// time is that of the memory either way (ResNet-50, 8 workers: 178 us both).
+__device__ __forceinline__ float mx4_mean(int32_t sum, double half, const Mx4Mean& by)
 {
-    // 2^(byte - 128) = 2^(byte - 1 - 127): exact, below 2^-126 as a denormal
-    const float half = byte > 1u ? __uint_as_float((byte - 1u) << 23) : __uint_as_float(byte == 1u ? 0x00400000u
-                                                                                               : 0x00200000u);
-    return byte == kMxNaN ? __uint_as_float(0x7FC00000u) : half * inv_m;
+    const double s = sum, q = s * by.inv_m;
+    return static_cast<float>(__builtin_fma(__builtin_fma(-q, by.m, s), by.inv_m, q) * half);
+}
+// 2^(byte - 128) for a byte of 1 and up.
+__device__ __forceinline__ double mx4_half(uint32_t byte)
+{
+    const uint64_t bits = byte == kMxNaN ? 0x7FF8000000000000u : static_cast<uint64_t>(byte + 1023u - 128u) << 52;
+    return __builtin_bit_cast(double, bits);
 }
 
 // Eight results of each lane, stored: a wave's 512 coordinates from `first` on.
@@ -460,7 +476,7 @@ __device__ __forceinline__ void store_octets(V* to, int64_t first, int64_t d, in
 
 // The mean (with out) of the sums and their stores.
 template <bool NT>
-__device__ __forceinline__ void finish_octet(const int32_t (&total)[8], uint32_t byte, float inv_m, int64_t first,
+__device__ __forceinline__ void finish_octet(const int32_t (&total)[8], uint32_t byte, const Mx4Mean& by, int64_t first,
                                              int64_t d, int lane, int32_t* sum, float* out)
 {
     uint32_t r[8];
@@ -470,10 +486,10 @@ __device__ __forceinline__ void finish_octet(const int32_t (&total)[8], uint32_t
     store_octets<NT>(sum, first, d, lane, r);
     if (out == nullptr)
         return;
-    const float deq = mx4_mean_factor(byte, inv_m);
+    const double half = mx4_half(byte);
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-        r[j] = __float_as_uint(static_cast<float>(total[j]) * deq);
+        r[j] = __float_as_uint(mx4_mean(total[j], half, by));
     store_octets<NT>(out, first, d, lane, r);
 }
 
@@ -482,7 +498,7 @@ __device__ __forceinline__ void finish_octet(const int32_t (&total)[8], uint32_t
 // LOADS: gradients read nontemporally.
 template <int ROWS, bool NT, bool LOADS>
 __global__ __launch_bounds__(kBlock) void k_mx4_step(const float* g, int64_t d, int32_t rows, int64_t ldg,
-                                                     uint64_t seed, uint8_t* scales, int32_t* sum, float inv_m,
+                                                     uint64_t seed, uint8_t* scales, int32_t* sum, Mx4Mean by,
                                                      float* out, int64_t oct0, int64_t octs)
 {
     const int lane = threadIdx.x & 63;
@@ -525,7 +541,7 @@ __global__ __launch_bounds__(kBlock) void k_mx4_step(const float* g, int64_t d, 
         for (int j = 0; j < 8; ++j)
             total[j] = 0;
     }
-    finish_octet<NT>(total, byte, inv_m, (o - lane) * 8, d, lane, sum, out);
+    finish_octet<NT>(total, byte, by, (o - lane) * 8, d, lane, sum, out);
 }
 
 // The whole step with the rows of 512 coordinates spread over a block's four
@@ -533,7 +549,7 @@ __global__ __launch_bounds__(kBlock) void k_mx4_step(const float* g, int64_t d, 
 // sums through LDS.  1000 coordinates of 8 workers 3.4 us, 6.4 with a wave for
 // all rows.
 __global__ __launch_bounds__(kBlock) void k_mx4_step_spread(const float* g, int64_t d, int32_t rows, int64_t ldg,
-                                                         uint64_t seed, uint8_t* scales, int32_t* sum, float inv_m,
+                                                         uint64_t seed, uint8_t* scales, int32_t* sum, Mx4Mean by,
                                                          float* out, int64_t oct0, int64_t octs)
 {
     constexpr int kWaves = kBlock / 64, kEach = 16 / kWaves;
@@ -592,14 +608,14 @@ __global__ __launch_bounds__(kBlock) void k_mx4_step_spread(const float* g, int6
         for (int j = 0; j < 8; ++j)
             total[j] = 0;
     }
-    finish_octet<false>(total, byte, inv_m, (o - lane) * 8, d, lane, sum, out);
+    finish_octet<false>(total, byte, by, (o - lane) * 8, d, lane, sum, out);
 }
 
 // The rows' codes on given bytes, added into sum (= or +=), and with out the mean.
 template <bool NT>
 __global__ __launch_bounds__(kBlock) void k_mx4_sum(const float* g, int64_t d, int32_t rows, int64_t ldg,
                                                     int32_t worker0, const uint8_t* scales, uint64_t seed,
-                                                    int32_t accumulate, int32_t* sum, float inv_m, float* out,
+                                                    int32_t accumulate, int32_t* sum, Mx4Mean by, float* out,
                                                     int64_t oct0, int64_t octs)
 {
     const int lane = threadIdx.x & 63;
@@ -638,7 +654,7 @@ __global__ __launch_bounds__(kBlock) void k_mx4_sum(const float* g, int64_t d, i
                 total[j] += bytes.total(j, held);
         }
     }
-    finish_octet<NT>(total, byte, inv_m, (o - lane) * 8, d, lane, sum, out);
+    finish_octet<NT>(total, byte, by, (o - lane) * 8, d, lane, sum, out);
 }
 
 int64_t blocks_for(int64_t units, int64_t per)
@@ -771,10 +787,10 @@ hipError_t launch_mx4_quantize_sum(const float* g, int64_t d, int32_t rows, int6
                                    const uint8_t* scales, uint64_t seed, int32_t accumulate, int32_t* sum, int32_t M,
                                    float* out, hipStream_t stream)
 {
-    const float inv_m = out != nullptr ? 1.0f / static_cast<float>(M) : 0.0f;
+    const Mx4Mean by = {static_cast<double>(M), out != nullptr ? 1.0 / M : 0.0};
     const auto kernel = 4 * d > kMxNontemporalBytes ? k_mx4_sum<true> : k_mx4_sum<false>;
     return over_octets(d, kBlock, [&](int64_t o, int64_t octs, unsigned grid) {
-        kernel<<<grid, kBlock, 0, stream>>>(g, d, rows, ldg, worker0, scales, seed, accumulate, sum, inv_m, out, o,
+        kernel<<<grid, kBlock, 0, stream>>>(g, d, rows, ldg, worker0, scales, seed, accumulate, sum, by, out, o,
                                             octs);
     });
 }
@@ -799,13 +815,13 @@ static auto step_kernel(int32_t rows)
 hipError_t launch_mx4_aggregate(const float* g, int64_t d, int32_t M, int64_t ldg, uint64_t seed, uint8_t* scales,
                                 int32_t* sum, float* out, hipStream_t stream)
 {
-    const float inv_m = 1.0f / static_cast<float>(M);
+    const Mx4Mean by = {static_cast<double>(M), 1.0 / M};
     const bool spread = 4 * d <= kMxNontemporalBytes && (M >= 5 || d <= kMxSpread);
     const auto kernel = spread ? k_mx4_step_spread
                       : 4 * d <= kMxNontemporalBytes ? step_kernel<false, false>(M)
                       : 4 * d * M <= kMxStreamBytes ? step_kernel<true, false>(M) : step_kernel<true, true>(M);
     return over_octets(d, spread ? 64 : kBlock, [&](int64_t o, int64_t octs, unsigned grid) {
-        kernel<<<grid, kBlock, 0, stream>>>(g, d, M, ldg, seed, scales, sum, inv_m, out, o, octs);
+        kernel<<<grid, kBlock, 0, stream>>>(g, d, M, ldg, seed, scales, sum, by, out, o, octs);
     });
 }
 
