@@ -805,11 +805,17 @@ constexpr int64_t kMxStreamBytes = int64_t(256) << 20;
 // 181.0 and 176.6; 2 rows of 262,144 3.0 either way, of 1.05 M 5.4 and 4.3.
 constexpr int64_t kMxSpread = int64_t(1) << 18;
 
-template <bool NT, bool LOADS>
+// MOST: the rows that calls of these stores and loads have.
+template <bool NT, bool LOADS, int MOST>
 static auto step_kernel(int32_t rows)
 {
-    return rows <= 2 ? k_mx4_step<2, NT, LOADS> : rows <= 4 ? k_mx4_step<4, NT, LOADS>
-         : rows <= 8 ? k_mx4_step<8, NT, LOADS> : k_mx4_step<16, NT, LOADS>;
+    if constexpr (MOST > 8)
+        if (rows > 8)
+            return k_mx4_step<16, NT, LOADS>;
+    if constexpr (MOST > 4)
+        if (rows > 4)
+            return k_mx4_step<8, NT, LOADS>;
+    return rows > 2 ? k_mx4_step<4, NT, LOADS> : k_mx4_step<2, NT, LOADS>;
 }
 
 hipError_t launch_mx4_aggregate(const float* g, int64_t d, int32_t M, int64_t ldg, uint64_t seed, uint8_t* scales,
@@ -817,9 +823,11 @@ hipError_t launch_mx4_aggregate(const float* g, int64_t d, int32_t M, int64_t ld
 {
     const Mx4Mean by = {static_cast<double>(M), 1.0 / M};
     const bool spread = 4 * d <= kMxNontemporalBytes && (M >= 5 || d <= kMxSpread);
+    // not spread, plain stores: at most 4 rows; outputs past 46 MiB and gradients
+    // up to 256 MiB: at most 5
     const auto kernel = spread ? k_mx4_step_spread
-                      : 4 * d <= kMxNontemporalBytes ? step_kernel<false, false>(M)
-                      : 4 * d * M <= kMxStreamBytes ? step_kernel<true, false>(M) : step_kernel<true, true>(M);
+                      : 4 * d <= kMxNontemporalBytes ? step_kernel<false, false, 4>(M)
+                      : 4 * d * M <= kMxStreamBytes ? step_kernel<true, false, 5>(M) : step_kernel<true, true, 16>(M);
     return over_octets(d, spread ? 64 : kBlock, [&](int64_t o, int64_t octs, unsigned grid) {
         kernel<<<grid, kBlock, 0, stream>>>(g, d, M, ldg, seed, scales, sum, by, out, o, octs);
     });
