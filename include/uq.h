@@ -488,9 +488,10 @@ int uq_mx4_dequantize(const uint8_t* codes, int64_t ldc, const uint8_t* scales, 
  * out[i][j] = sum over l < k of A[i][l] * B[j][l] for two matrices held as
  * codes whose blocks run along l (both operands row by row: B is the second
  * factor transposed, as a layer's weight [outputs][inputs] lies).  Products of
- * elements and scales are exact, sums are binary32 in an order that depends
- * on the sizes and leading dimensions alone.  A block of byte 255 makes the outputs of its row or
- * column NaN.
+ * elements and scales are exact, sums are binary32 (denormals kept) in an order
+ * that depends on the sizes and leading dimensions alone; where a product or a
+ * partial sum passes the largest binary32 the output may be infinite or NaN.  A
+ * block of byte 255 makes the outputs of its row or column NaN.
  *   a, lda, a_scales, ldas   m x k codes      b, ldb, b_scales, ldbs   n x k codes
  *   m, n, k      0 .. 2^31 - 1 (k = 0: the sum is 0)
  *   type         of out
