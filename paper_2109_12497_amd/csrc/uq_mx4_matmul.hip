@@ -41,7 +41,7 @@ int64_t tile_blocks(int64_t m, int64_t n, MatmulPlan::Form form)
 //
 // Tiles, `stages` stages of 256 deep: a stage costs more with more compute units
 // at work, for they share the caches' bandwidth and then run slower.  8192^3
-// 267 us in tiles of 256 x 256; 2048^3 10.7 us in 128 x 128, 19 in 256 x 256; 192 x
+// 260 us in tiles of 256 x 256; 2048^3 10.7 us in 128 x 128, 19 in 256 x 256; 192 x
 // 4096 x 4096 10.9 in 64 x 128, 14.0 in 128 x 128.
 double tiles_ns(int64_t m, int64_t n, int64_t stages, int64_t parts, MatmulPlan::Form form)
 {
@@ -400,12 +400,13 @@ struct Operand {
 // instruction t = 0..3: any order of the blocks along k gives the same
 // products as long as both operands keep to it, and in this one a lane's four
 // scale bytes are one dword.
-//   What bounds it, 8192^3 to bf16 on one MI355X: 261 us, 4210 TFLOP/s.  The
+//   What bounds it, 8192^3 to bf16 on one MI355X: 261 us, 4210 TFLOP/s (three
+// sets of operands in turn, the card warm; 257 to 265 from card to card).  The
 // card lowers its clock by the data: on zeros the same instructions take 187
 // us (5890), and matrix instructions alone reach 6540 on random codes and 9000
 // on zeros.  The rest is the loads into LDS (without them, on random codes, 15%
 // less), and the outputs, which all compute units store at once (4%).  Eight
-// waves of 128 x 64 against four of 128 x 128: 269 and 272 us.
+// waves of 128 x 64 against four of 128 x 128: 1% less time.
 template <int T, int WM, int WN, int FM, int FN, int NS>
 __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx4_tiles(MatmulArgs g)
 {
@@ -593,15 +594,15 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx4_tiles(MatmulArgs g)
     const bool add = g.accumulate != 0;
     Four<T> old[3][kTurns];
     // Large tiles read them nontemporally (8192^3 added to bf16, outputs in turn,
-    // 303 us, 326 otherwise; 4096 x 4096 x 8192 to fp32 92 either way), small ones not
-    // (1000 x 3000 x 700 11.7 and 10.5).
-    constexpr bool kPast = BM * BN >= 256 * 256;
+    // 291 us, 312 otherwise, one output each time 289 and 281; 4096 x 4096 x 8192 to
+    // fp32 87 and 82 either way), small ones not (1000 x 3000 x 700 11.7 and 10.5).
+    constexpr bool kReadPast = BM * BN >= 256 * 256;
     const auto load_old = [&](int i) {
 #pragma unroll
         for (int r = 0; r < kTurns; ++r) {
             const int64_t row = first + 32 * i + r * (64 / kLanes);
             if (row < g.m)
-                old[i % 3][r] = load_four<T, kPast>(out, row * g.ldo, col, g.n);
+                old[i % 3][r] = load_four<T, kReadPast>(out, row * g.ldo, col, g.n);
         }
     };
     if (add) {
@@ -898,10 +899,14 @@ hipError_t product(const MatmulArgs& g, const MatmulPlan& plan, float* ws, hipSt
 
 }  // namespace
 
-// Outputs from half the Infinity Cache's size on pass it by: 8192 x 4096 x 4096
-// added to fp32 (134 MB), three outputs in turn, 125 us, 141 otherwise (one output
-// each time 124 and 110); 4096 x 4096 x 8192 (67 MB) 94 either way, and 94 and
-// 89; 8192^3 to bf16 (134 MB), outputs in turn, 277 and 294.
+// Outputs from half the Infinity Cache's size on pass it by.  With three outputs
+// in turn 8192^3 to bf16 (134 MB) takes 261 us, 277 otherwise, added to 291 and 304,
+// 65536 x 1024 x 1024 60 and 75, 8192 x 4096 x 4096 added to fp32 (134 MB) 122 and 127; one
+// output each time 259 and 263, 289 and 280, 59 and 64, 122 and 107.  What loses
+// is a product added to one output again and again with nothing in between; a
+// layer of 8192 x 8192 and 8192 rows (bf16, its own y and dw each time, dw added to)
+// takes 310 us forward, 335 otherwise, and 681 backward, 717.  4096 x 4096 x 8192 (67 MB)
+// lost 5% with one output and gained nothing with three.
 constexpr double kPastBytes = 128.0 * (1 << 20);
 
 static size_t parts_bytes(const MatmulPlan& plan, int64_t m, int64_t n)

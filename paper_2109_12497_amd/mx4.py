@@ -96,7 +96,8 @@ class Mx4Linear:
     rounds a layer's dy and then the dy formed from it, the second rounding
     depends on what it rounds and the chain is biased.  y, dx and dw are views of the layer's own buffers (y
     and dx of `dtype`, dw in binary32) and stay until the next call that
-    writes them.  Calls allocate nothing: the workspace is sized once, for the
+    writes them.  Rows of x, w and dy start on 16-byte boundaries, and the layer
+    is called by hand: it takes no part in autograd.  Calls allocate nothing: the workspace is sized once, for the
     number of rows that needs the most.
     """
 
