@@ -825,6 +825,7 @@ hipError_t launch_mx4_aggregate(const float* g, int64_t d, int32_t M, int64_t ld
     const bool spread = 4 * d <= kMxNontemporalBytes && (M >= 5 || d <= kMxSpread);
     // not spread, plain stores: at most 4 rows; outputs past 46 MiB and gradients
     // up to 256 MiB: at most 5
+    static_assert(6 * kMxNontemporalBytes >= kMxStreamBytes, "six rows past the one are past the other");
     const auto kernel = spread ? k_mx4_step_spread
                       : 4 * d <= kMxNontemporalBytes ? step_kernel<false, false, 4>(M)
                       : 4 * d * M <= kMxStreamBytes ? step_kernel<true, false, 5>(M) : step_kernel<true, true, 16>(M);
